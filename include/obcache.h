@@ -76,7 +76,8 @@ typedef enum {
 
 typedef enum {
     OBC_F32 = 0,   /* q,k,v fp32; head_dim 64 or 128; fp32 arithmetic */
-    OBC_BF16 = 1   /* q,k,v bf16; head_dim 64 or 128; fp32 accumulation */
+    OBC_BF16 = 1,  /* q,k,v bf16; head_dim 64 or 128; fp32 accumulation */
+    OBC_E4M3 = 2   /* rows of an obc_cache_t only: 8-bit numbers with a power of two per 32 channels, see there */
 } obc_dtype_t;
 
 #define OBC_MAX_RAGGED_BATCH 128  /* largest B accepted together with seq_lens_host */
@@ -306,6 +307,98 @@ int obc_decode_step(const void *q, void *k, void *v, float *scores, int32_t *evi
  */
 int obc_compact_scores(const float *scores, const int32_t *keep_idx, float *scores_out,
                        int B, int Hkv, int N, int budget, int N_out, void *hip_stream);
+
+/*
+ * The cache that kept and new rows live in.  The calls above score, select and compact; the three below write rows into a
+ * cache (obc_cache_append), attend over it (obc_attend) and give rows back in the layout of the calls above
+ * (obc_cache_read).  The struct is HOST memory, read before a call returns; what it points to is device memory.
+ *   k, v        [num_pages, Hkv, page_size, d] of `dtype`
+ *   page_table  [batch, pages_per_seq] int32: row j of sequence b lies in slot j % page_size of page
+ *               page_table[b][j / page_size].  page_size is then a power of two.  Or NULL: page b holds all rows of
+ *               sequence b (num_pages = batch, pages_per_seq = 1, any page_size), which is the [B, Hkv, N, d] cache of
+ *               the calls above with N = page_size.
+ *   dtype       OBC_F32, OBC_BF16 or OBC_E4M3; d 64 or 128
+ *   k_scale, v_scale  [num_pages, Hkv, page_size, d / 32] bytes, OBC_E4M3 only (NULL otherwise): e + 127 for each 32
+ *               channels of a row, whose values are code * 2^e, the codes 8-bit floating-point numbers of four
+ *               exponent and three mantissa bits (no infinities, largest 448).  e is the least integer for which no finite value
+ *               of the block exceeds 448 * 2^e, at least -117; codes are rounded to nearest even; infinities and NaN become
+ *               NaN.  Every stored value is exact in bf16, and a row read back and stored again keeps its values.
+ * Alignment: k, v 16 bytes, scales and tables 4.  pages_per_seq * page_size <= OBC_MAX_CACHE_ROWS, batch * Hkv <= 65535.
+ * Page numbers are device data that is not checked on the host: a number outside the pool is taken as the nearest inside by calls
+ * that read, and rows that would be written there are dropped.  Several sequences may read one page; what a
+ * place holds that one call writes twice is unspecified.
+ *
+ * Lengths are DEVICE data as well, so that a captured step can be replayed as the cache grows:
+ *   lens      int32 [B], or [B, Hkv] with lens_per_head = 1 (a head-adaptive eviction's `counts`): rows in the cache, the new
+ *             ones included.  As everywhere in this file the new rows are the last ones.
+ *   new_lens  int32 [B] or NULL: how many of the T rows of a padded chunk are new rows of sequence b (NULL: all T); the first of
+ *             them count.  Brought into [0, T].
+ * A row index is not a position: after an eviction a row has moved, so the rotation takes positions of its own.
+ */
+#define OBC_MAX_CACHE_ROWS (1 << 30)
+typedef struct {
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+    const int32_t *page_table;
+    int32_t batch, num_pages, pages_per_seq, page_size, Hkv, d, dtype;
+} obc_cache_t;
+
+/* Rows of d contiguous elements at data + b * batch_stride + t * token_stride + h * head_stride (elements; not negative,
+ * multiples of 16 bytes; data 16-byte aligned): [B, T, H, d] in any order of its first three dimensions, a slice of a fused
+ * projection's output included. */
+typedef struct {
+    const void *data;
+    int64_t batch_stride, token_stride, head_stride;
+} obc_rows_t;
+
+/*
+ * New rows: norm, rotation and write in one pass.  For t < n_b (new_lens[b], or T), in fp32 with one rounding at the end:
+ *   1. q_norm, k_norm ([d] of `dtype`, 16-byte aligned, or NULL): x <- x / sqrt(mean(x^2) + eps) * w over each head's d channels;
+ *   2. rot_pairs > 0: channel pairs (i, i + rot_pairs), or (2i, 2i + 1) with interleaved = 1, of q and k are turned:
+ *      (x, y) <- rot_scale * (x cos a - y sin a, y cos a + x sin a), a = positions[b, t] * inv_freq[i], the angle
+ *      reduced in 64 bits.  positions int32 [B, T], inv_freq fp32 [rot_pairs]; the channels from 2 * rot_pairs up are
+ *      left as they are.  (Frequencies and rot_scale carry whatever scaling a longer context asks for.)  rot_pairs is a
+ *      multiple of 8 and at most d / 2.
+ *   3. k and v go to row lens[b (, g)] - n_b + t of the cache, q to q_out [B, Hq, T, d], the layout that obc_score and obc_attend
+ *      take.  Rows that would lie before row 0 or past the cache's end are dropped.
+ * Rows t >= n_b are not written to the cache and are zero in q_out.
+ * q may be NULL (with q_out, q_norm NULL and Hq 0): rows that are stored as they are, such as those an eviction kept; only then
+ * may new_lens be [B, Hkv] (new_lens_per_head = 1: the lists of obc_select_adaptive).
+ * `dtype` (OBC_F32 or OBC_BF16) is the inputs'; the cache's is the same or OBC_E4M3.
+ */
+int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t *v, const obc_cache_t *cache, void *q_out,
+                     const int32_t *lens, int lens_per_head, const int32_t *new_lens, int new_lens_per_head,
+                     const int32_t *positions, const float *inv_freq, int rot_pairs, float rot_scale, int interleaved,
+                     const void *q_norm, const void *k_norm, float eps, int B, int T, int Hq, int dtype, void *hip_stream);
+
+/*
+ * Attention of the new rows over the cache:
+ *   out[b,t,h,:] = sum_j p_j v_j,  p = softmax_j(scale * q[b,h,t].k_j)
+ * over the rows j < lens - n_b + t + 1 of KV head h / (Hq/Hkv) (causal = 1: a new row sees what was there and the new
+ * rows up to itself), or over all j < lens (causal = 0: cross attention).  T = 1 is a decoding step, a larger T a chunk of a prompt.
+ *   q    [B, Hq, T, d] of `dtype` (OBC_F32 or OBC_BF16); the cache is of the same type or OBC_E4M3
+ *   out  [B, T, Hq, d] of `dtype` (what the output projection takes), written in full: rows t >= n_b, and rows that see
+ *        nothing, are 0.  Must not alias the inputs.
+ * lens is brought into [0, pages_per_seq * page_size].  Rows of the cache from lens on, pages that only hold such rows, and rows
+ * t >= n_b of q may hold anything; NaN or an infinity in the first `lens` rows gives undefined results for that KV head.
+ * Products are summed in fp32.  With bf16 queries the weights are rounded to bf16 before they meet v.
+ * scale > 0 (1/sqrt(d) is the usual one).  workspace: obc_attend_workspace_bytes(...) bytes, 256-byte aligned (none needed where
+ * that is 0).  Calls that may run at the same time need workspaces of their own.
+ */
+int obc_attend_workspace_bytes(int B, int T, int Hq, const obc_cache_t *cache, int dtype, size_t *bytes_out);
+int obc_attend(const void *q, const obc_cache_t *cache, void *out, const int32_t *lens, int lens_per_head, const int32_t *new_lens,
+               int B, int T, int Hq, int dtype, int causal, float scale, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Rows of the cache, in the layout of the calls above:
+ *   k_out[b,g,j,:] = row keep_idx[b,g,j] (NULL: row j) of KV head g of sequence b, and the same for v.
+ *   keep_idx      [B, Hkv, n] int32 or NULL (then n <= pages_per_seq * page_size); -1 gives an all-zero row, entries past the
+ *                 cache's end are clamped to its last row, as in obc_compact
+ *   k_out, v_out  [B, Hkv, n, d] of `dtype`: the cache's own, or OBC_F32 or OBC_BF16 for an OBC_E4M3 cache
+ * With the indices of obc_select* it is obc_compact for paged and 8-bit caches; obc_cache_append stores the result again.
+ */
+int obc_cache_read(const obc_cache_t *cache, const int32_t *keep_idx, void *k_out, void *v_out, int B, int n, int dtype,
+                   void *hip_stream);
 
 /* ------------------------------------------------------------------------------------
  * Measurement and test hooks.  None of these is part of the method; a caller of the

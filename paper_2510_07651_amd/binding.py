@@ -17,13 +17,25 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libobcache.so")
 
 OBC_VALUE, OBC_KEY, OBC_JOINT, OBC_ALL, OBC_ATTN, OBC_VATP = 0, 1, 2, 3, 4, 5
-OBC_F32, OBC_BF16 = 0, 1
+OBC_F32, OBC_BF16, OBC_E4M3 = 0, 1, 2
 OBC_OK, OBC_EINVAL, OBC_EUNSUPPORTED, OBC_EWORKSPACE, OBC_ELAUNCH = 0, -1, -2, -3, -4
 VARIANT_CODES = {"value": OBC_VALUE, "key": OBC_KEY, "joint": OBC_JOINT, "all": OBC_ALL, "attn": OBC_ATTN,
                  "vatp": OBC_VATP}
 
 _lib = None
 _F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+_E4M3, _U8 = torch.float8_e4m3fn, torch.uint8
+
+
+class _CacheArg(ctypes.Structure):
+    """obc_cache_t"""
+    _fields_ = ([(x, ctypes.c_void_p) for x in ("k", "v", "k_scale", "v_scale", "page_table")]
+                + [(x, ctypes.c_int32) for x in ("batch", "num_pages", "pages_per_seq", "page_size", "Hkv", "d", "dtype")])
+
+
+class _RowsArg(ctypes.Structure):
+    """obc_rows_t"""
+    _fields_ = [("data", ctypes.c_void_p)] + [(x, ctypes.c_int64) for x in ("batch_stride", "token_stride", "head_stride")]
 
 
 class ObcError(RuntimeError):
@@ -95,6 +107,17 @@ def load_library():
     lib.obc_set_score_tuning.argtypes = [c_int, c_int]
     lib.obc_set_sweep2_form.restype = c_int
     lib.obc_set_sweep2_form.argtypes = [c_int]
+    cache_p, rows_p, c_float = ctypes.POINTER(_CacheArg), ctypes.POINTER(_RowsArg), ctypes.c_float
+    lib.obc_cache_append.restype = c_int
+    lib.obc_cache_append.argtypes = [rows_p, rows_p, rows_p, cache_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p,
+                                     c_int, c_float, c_int, c_void_p, c_void_p, c_float, c_int, c_int, c_int, c_int, c_void_p]
+    lib.obc_attend_workspace_bytes.restype = c_int
+    lib.obc_attend_workspace_bytes.argtypes = [c_int, c_int, c_int, cache_p, c_int, ctypes.POINTER(c_size_t)]
+    lib.obc_attend.restype = c_int
+    lib.obc_attend.argtypes = [c_void_p, cache_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_int, c_int, c_float,
+                               c_void_p, c_size_t, c_void_p]
+    lib.obc_cache_read.restype = c_int
+    lib.obc_cache_read.argtypes = [cache_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p]
     _lib = lib
     return lib
 
@@ -480,6 +503,215 @@ def obc_compact_scores(scores: torch.Tensor, keep_idx: torch.Tensor, n_out: Opti
     if rc != OBC_OK:
         raise ObcError(rc, "obc_compact_scores")
     return scores_out
+
+
+class KvCache:
+    """The cache of one layer that obc_cache_append, obc_attend and obc_cache_read work on.
+
+    k, v [P,Hkv,S,d] float32, bfloat16 or float8_e4m3fn, the latter with k_scale, v_scale [P,Hkv,S,d/32] uint8; page_table [B,M]
+    int32, or None: page b is all of sequence b, so that the library's [B,Hkv,N,d] caches serve as they are.  Tensors are
+    checked here, once; the handle keeps them and their addresses."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: Optional[torch.Tensor] = None,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        _require_cuda(k, v)
+        if k.dim() != 4 or v.shape != k.shape or v.dtype is not k.dtype or v.device != k.device:
+            raise ValueError("k, v must be [P,Hkv,S,d] of one type")
+        codes = {_F32: OBC_F32, _BF16: OBC_BF16, _E4M3: OBC_E4M3}
+        if k.dtype not in codes:
+            raise TypeError("a cache is float32, bfloat16 or float8_e4m3fn, got %s" % k.dtype)
+        P, Hkv, S, d = k.shape
+        if 0 in k.shape or d not in (64, 128):
+            raise ValueError("a cache has pages, heads and rows of 64 or 128 channels")
+        if k.dtype is _E4M3:
+            for x in (k_scale, v_scale):
+                if x is None or x.dtype is not _U8 or tuple(x.shape) != (P, Hkv, S, d // 32) or x.device != k.device:
+                    raise ValueError("an 8-bit cache needs k_scale, v_scale [P,Hkv,S,%d] uint8" % (d // 32))
+                _require_cuda(x)
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("scales belong to an 8-bit cache")
+        if page_table is not None:
+            _require_cuda(page_table)
+            if page_table.dim() != 2 or page_table.dtype is not _I32 or page_table.device != k.device or 0 in page_table.shape:
+                raise ValueError("page_table must be [B,M] int32")
+            if S & (S - 1):
+                raise ValueError("pages of a table hold a power of two of rows")
+        self.k, self.v, self.k_scale, self.v_scale, self.page_table = k, v, k_scale, v_scale, page_table
+        self.batch, pages = (P, 1) if page_table is None else tuple(page_table.shape)
+        self.Hkv, self.d, self.dtype, self.device = Hkv, d, k.dtype, k.device
+        self.capacity = pages * S
+        if self.capacity > 1 << 30 or self.batch * Hkv > 65535:
+            raise ValueError("at most 2^30 rows per sequence and 65535 KV heads over the batch")
+        self._index = k.get_device()
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._arg = _CacheArg(ptr(k), ptr(v), ptr(k_scale), ptr(v_scale), ptr(page_table), self.batch, P, pages, S, Hkv, d, codes[k.dtype])
+        self._ref = ctypes.pointer(self._arg)
+
+    @classmethod
+    def empty(cls, num_pages: int, Hkv: int, page_size: int, d: int, dtype=torch.bfloat16, page_table=None, device="cuda"):
+        """A cache of its own memory, not initialised."""
+        k, v = (torch.empty((num_pages, Hkv, page_size, d), dtype=dtype, device=device) for _ in range(2))
+        ks = vs = None
+        if dtype is _E4M3:
+            ks, vs = (torch.empty((num_pages, Hkv, page_size, d // 32), dtype=_U8, device=device) for _ in range(2))
+        return cls(k, v, page_table, ks, vs)
+
+    def _ints(self, t: torch.Tensor, what: str, per_head: bool = True) -> int:
+        """1 for lengths [B,Hkv], 0 for [B]."""
+        if t.dtype is _I32 and t.get_device() == self._index and t.is_contiguous() and t.is_cuda:
+            if t.shape == (self.batch,):
+                return 0
+            if per_head and t.shape == (self.batch, self.Hkv):
+                return 1
+        raise ValueError("%s must be contiguous int32 [B]%s on the cache's GPU" % (what, " or [B,Hkv]" if per_head else ""))
+
+    def _launch(self, call, *args):
+        """call(*args, stream) on the current stream of the cache's GPU, with that one current."""
+        index = self._index
+        if index == torch.cuda.current_device():
+            return call(*args, _raw_stream(index) if _raw_stream is not None else _stream_ptr(self.k))
+        with torch.cuda.device(index):
+            return call(*args, _stream_ptr(self.k))
+
+
+def _rows(t: torch.Tensor, heads: Optional[int], like: torch.Tensor, what: str) -> _RowsArg:
+    B, T, _, d = like.shape
+    if (t.dim() != 4 or t.shape[0] != B or t.shape[1] != T or t.shape[3] != d or heads is not None and t.shape[2] != heads
+            or t.dtype is not like.dtype or t.get_device() != like.get_device() or not t.is_cuda):
+        raise ValueError("%s must be [B,T,H,d] and fit the other rows and the cache" % what)
+    sb, st, sh, sd = t.stride()
+    if sd != 1 and d != 1:
+        raise ValueError("%s: the channels of a row must be contiguous" % what)
+    return _RowsArg(t.data_ptr(), sb, st, sh)
+
+
+def obc_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, q: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None, new_lens: Optional[torch.Tensor] = None,
+                     positions: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, rot_scale: float = 1.0,
+                     interleaved: bool = False, q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+                     eps: float = 1e-6) -> Optional[torch.Tensor]:
+    """k, v [B,T,Hkv,d] (and q [B,T,Hq,d]), any strides over whole rows, normed, rotated and written: k, v to rows lens - n .. lens - 1
+    of the cache, q to q_out [B,Hq,T,d], which is returned.  lens [B] or [B,Hkv] int32 counts the new rows in; new_lens [B] int32
+    (without q also [B,Hkv]): the first n of the T are new; positions [B,T] int32 and inv_freq [pairs] float32 turn on the rotation."""
+    if k.dim() != 4 or k.shape[0] != cache.batch or k.shape[2] != cache.Hkv or k.shape[3] != cache.d or k.get_device() != cache._index:
+        raise ValueError("k must be [B,T,Hkv,d] on the cache's GPU")
+    if k.dtype is not cache.dtype and cache.dtype is not _E4M3:
+        raise ValueError("rows and cache must be of one type, or the cache of 8 bits")
+    B, T, _, d = k.shape
+    k_arg, v_arg = _rows(k, cache.Hkv, k, "k"), _rows(v, cache.Hkv, k, "v")
+    per_head = cache._ints(lens, "lens")
+    new_ptr, new_per_head = (None, 0) if new_lens is None else (new_lens.data_ptr(), cache._ints(new_lens, "new_lens", q is None))
+    q_arg, Hq = None, 0
+    if q is not None:
+        q_arg = ctypes.byref(_rows(q, None, k, "q"))
+        Hq = q.shape[2]
+        if Hq < 1 or Hq % cache.Hkv:
+            raise ValueError("q needs a multiple of Hkv heads")
+        if q_out is None:
+            q_out = torch.empty((B, Hq, T, d), dtype=k.dtype, device=k.device)
+        elif q_out.shape != (B, Hq, T, d) or q_out.dtype is not k.dtype or q_out.get_device() != cache._index or not q_out.is_contiguous():
+            raise ValueError("q_out must be contiguous [B,Hq,T,d] of q's type")
+    elif q_out is not None or q_norm is not None:
+        raise ValueError("q_out and q_norm belong to q")
+    if (positions is None) != (inv_freq is None):
+        raise ValueError("positions and inv_freq belong together")
+    pairs = 0
+    if inv_freq is not None:
+        pairs = inv_freq.numel()
+        if (inv_freq.dtype is not _F32 or inv_freq.get_device() != cache._index or not inv_freq.is_contiguous() or positions.dtype is not _I32
+                or positions.shape != (B, T) or positions.get_device() != cache._index or not positions.is_contiguous() or pairs < 1):
+            raise ValueError("positions must be contiguous [B,T] int32, inv_freq [pairs] float32, on the cache's GPU")
+    for w in (q_norm, k_norm):
+        if w is not None and (w.shape != (d,) or w.dtype is not k.dtype or w.get_device() != cache._index or not w.is_contiguous()):
+            raise ValueError("q_norm, k_norm must be contiguous [d] of the rows' type")
+    rc = cache._launch((_lib or load_library()).obc_cache_append, q_arg, ctypes.byref(k_arg), ctypes.byref(v_arg), cache._ref,
+                       None if q_out is None else q_out.data_ptr(), lens.data_ptr(), per_head, new_ptr, new_per_head,
+                       None if positions is None else positions.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(), pairs,
+                       rot_scale, 1 if interleaved else 0, None if q_norm is None else q_norm.data_ptr(),
+                       None if k_norm is None else k_norm.data_ptr(), eps, B, T, Hq, OBC_BF16 if k.dtype is _BF16 else _dtype_code(k))
+    if rc != OBC_OK:
+        raise ObcError(rc, "obc_cache_append")
+    return q_out
+
+
+def obc_attend_workspace_bytes(B: int, T: int, Hq: int, cache: KvCache, dtype) -> int:
+    """dtype: the queries', a torch type or its code."""
+    out = ctypes.c_size_t(0)
+    code = {_F32: OBC_F32, _BF16: OBC_BF16}.get(dtype, dtype)
+    if not isinstance(code, int):
+        raise TypeError("queries are float32 or bfloat16, got %s" % dtype)
+    rc = load_library().obc_attend_workspace_bytes(B, T, Hq, cache._ref, code, ctypes.byref(out))
+    if rc != OBC_OK:
+        raise ObcError(rc, "obc_attend_workspace_bytes")
+    return int(out.value)
+
+
+def obc_attend(q: torch.Tensor, cache: KvCache, lens: torch.Tensor, new_lens: Optional[torch.Tensor] = None, causal: bool = True,
+               scale: Optional[float] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q [B,Hq,T,d] over the first lens rows of the cache, the last n of which are the new rows themselves -> out [B,T,Hq,d].
+    lens [B] or [B,Hkv] int32, new_lens [B] int32 (None: T); scale defaults to 1/sqrt(d)."""
+    if not (q.is_cuda and q.is_contiguous() and q.dim() == 4):
+        raise ValueError("tensors must be contiguous and on the GPU")
+    B, Hq, T, d = q.shape
+    if B != cache.batch or d != cache.d or q.get_device() != cache._index or 0 in q.shape or Hq % cache.Hkv:
+        raise ValueError("q must be [B,Hq,T,d] and fit the cache")
+    dtype = q.dtype
+    if dtype is not cache.dtype and cache.dtype is not _E4M3:
+        raise ValueError("queries and cache must be of one type, or the cache of 8 bits")
+    code = OBC_BF16 if dtype is _BF16 else _dtype_code(q)
+    per_head = cache._ints(lens, "lens")
+    if new_lens is not None:
+        cache._ints(new_lens, "new_lens", False)
+    if out is None:
+        out = torch.empty((B, T, Hq, d), dtype=dtype, device=q.device)
+    elif out.shape != (B, T, Hq, d) or out.dtype is not dtype or out.get_device() != cache._index or not out.is_contiguous():
+        raise ValueError("out must be contiguous [B,T,Hq,d] of q's type")
+    if workspace is None:
+        workspace = torch.empty(obc_attend_workspace_bytes(B, T, Hq, cache, code), dtype=_U8, device=q.device)
+    elif not (workspace.is_cuda and workspace.is_contiguous() and workspace.get_device() == cache._index):
+        raise ValueError("workspace must be contiguous and on the cache's GPU")
+    rc = cache._launch((_lib or load_library()).obc_attend, q.data_ptr(), cache._ref, out.data_ptr(), lens.data_ptr(), per_head,
+                       None if new_lens is None else new_lens.data_ptr(), B, T, Hq, code, 1 if causal else 0,
+                       d ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    if rc != OBC_OK:
+        raise ObcError(rc, "obc_attend")
+    return out
+
+
+def obc_cache_read(cache: KvCache, n: Optional[int] = None, keep_idx: Optional[torch.Tensor] = None, dtype=None,
+                   k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """Rows keep_idx [B,Hkv,n] int32 (None: the first n) of the cache -> (k_out, v_out) [B,Hkv,n,d] of the cache's type, or of an
+    8-bit cache as `dtype` (bfloat16 if neither that nor outputs are given)."""
+    if keep_idx is not None:
+        if (keep_idx.dim() != 3 or keep_idx.shape[:2] != (cache.batch, cache.Hkv) or keep_idx.dtype is not _I32
+                or not keep_idx.is_contiguous() or keep_idx.get_device() != cache._index):
+            raise ValueError("keep_idx must be contiguous [B,Hkv,n] int32 on the cache's GPU")
+        if n is not None and n != keep_idx.shape[2]:
+            raise ValueError("n and keep_idx disagree")
+        n = keep_idx.shape[2]
+    elif n is None:
+        raise ValueError("either n or keep_idx says which rows")
+    n = int(n)
+    if n < 1 or keep_idx is None and n > cache.capacity:
+        raise ValueError("the cache has rows 0 .. %d" % (cache.capacity - 1))
+    if dtype is None:
+        given = k_out if k_out is not None else v_out
+        dtype = given.dtype if given is not None else _BF16 if cache.dtype is _E4M3 else cache.dtype
+    if dtype is not cache.dtype and cache.dtype is not _E4M3 or dtype not in (_F32, _BF16):
+        raise ValueError("rows are given back in the cache's type, of an 8-bit cache in float32 or bfloat16")
+    shape = (cache.batch, cache.Hkv, n, cache.d)
+    outs = []
+    for x in (k_out, v_out):
+        if x is None:
+            x = torch.empty(shape, dtype=dtype, device=cache.device)
+        elif x.shape != shape or x.dtype is not dtype or x.get_device() != cache._index or not x.is_contiguous():
+            raise ValueError("k_out, v_out must be contiguous [B,Hkv,n,d] of one type on the cache's GPU")
+        outs.append(x)
+    rc = cache._launch((_lib or load_library()).obc_cache_read, cache._ref, None if keep_idx is None else keep_idx.data_ptr(),
+                       outs[0].data_ptr(), outs[1].data_ptr(), cache.batch, n, OBC_F32 if dtype is _F32 else OBC_BF16)
+    if rc != OBC_OK:
+        raise ObcError(rc, "obc_cache_read")
+    return outs[0], outs[1]
 
 
 OBC_PROBE_BLOCKS = 2048

@@ -1,0 +1,258 @@
+// Attention of new tokens over the cache: out = softmax(scale q k^T) v over the rows a token may see.
+//
+// The rows (new token t, query head h of a KV head) of one KV head read the same keys and values, so they are taken together,
+// token by token: row r is token r / G of query head g G + r % G, and a tile of consecutive rows sees nearly the same tokens.
+#include <type_traits>
+
+#include "cache.h"
+#include "mfma_util.h"
+#include "wave_util.h"
+
+namespace obc {
+namespace {
+
+using mfma::f32x16;
+
+constexpr float kNone = -3.0e38f;      // running maximum of a row that has seen nothing: finite, so that differences stay numbers
+
+// Tokens the rows of new token t see of a KV head with `len` rows, `n` of them new.
+__device__ __forceinline__ int tokens_seen(int len, int n, int t, int causal) {
+    if (t >= n) return 0;
+    return causal ? max(len - n + t + 1, 0) : len;
+}
+
+struct Tile {            // rows r0 .. r0 + size - 1 of KV head g of sequence b
+    int b, g, r0, len, n, seen;      // seen: the most any of its rows sees
+};
+__device__ __forceinline__ Tile tile_of(const AttendArgs &a, int bg, int r0, int size) {
+    Tile x;
+    x.b = bg / a.Hkv;
+    x.g = bg % a.Hkv;
+    x.r0 = r0;
+    x.len = min(max(device_len(a.lens, x.b, x.g, a.Hkv), 0), a.cache.capacity);
+    x.n = a.fresh ? min(max(a.fresh[x.b], 0), a.T) : a.T;
+    const int first = r0 / a.G, last = min((r0 + size - 1) / a.G, x.n - 1);
+    x.seen = first <= last ? tokens_seen(x.len, x.n, last, a.causal) : 0;
+    return x;
+}
+// Tokens per share of a tile: the same in the kernels that leave partial sums and in the one that joins them.
+__device__ __forceinline__ int share_of(int seen, int splits, int min_share) {
+    const int even = (seen + splits - 1) / splits;
+    return max((even + min_share - 1) / min_share * min_share, min_share);
+}
+
+template <int kDtype>
+__device__ __forceinline__ void store4(char *p, const float (&x)[4]) {
+    if constexpr (kDtype == OBC_BF16) *(u32x2 *)p = u32x2{bf16_pair_of(x[0], x[1]), bf16_pair_of(x[2], x[3])};
+    else *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]);
+}
+
+// The general kernel, in fp32: one wave per (tile of 32 rows, share).  S^T = K Q^T and O^T = V^T P^T on the fp32 matrix cores: a
+// lane holds one row's column of both, so the softmax needs one exchange between the wave's halves and no shuffle of P:
+// register 4 j + i of S^T is token 8 j + 4 half + i, and as long as V's operand takes its tokens in that order the product is the same.
+template <int kD, int kDtype, bool kCodes>
+__global__ __launch_bounds__(256) void attend_plain(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int units = plan.tiles * plan.splits * a.B * a.Hkv;
+    const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= units) return;
+    const int split = unit % plan.splits, tile = unit / plan.splits % plan.tiles, bg = unit / (plan.splits * plan.tiles);
+    const Tile x = tile_of(a, bg, tile * 32, 32);
+    const int share = share_of(x.seen, plan.splits, plan.min_share);
+    const int begin = split * share, end = min(begin + share, x.seen);
+    if (begin >= end && split > 0) return;
+
+    constexpr int kSize = kDtype == OBC_BF16 ? 2 : 4;
+    const int row = x.r0 + col, t = row / a.G, h = x.g * a.G + row % a.G;
+    const bool exists = t < a.T;
+    const int seen = exists ? tokens_seen(x.len, x.n, t, a.causal) : 0;
+    float q[kD / 2];             // channels 8 s + 4 half + i
+    const char *q_row = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * (kD * kSize);
+#pragma unroll
+    for (int s = 0; s < kD / 8; ++s) {
+        const char *p = q_row + (8 * s + 4 * half) * kSize;
+        if constexpr (kDtype == OBC_BF16) {
+            const u32x2 w = *(const u32x2 *)p;
+            q[4 * s] = __uint_as_float(w[0] << 16); q[4 * s + 1] = __uint_as_float(w[0] & 0xffff0000u);
+            q[4 * s + 2] = __uint_as_float(w[1] << 16); q[4 * s + 3] = __uint_as_float(w[1] & 0xffff0000u);
+        } else {
+            *(float4 *)(q + 4 * s) = *(const float4 *)p;
+        }
+    }
+    f32x16 o[kD / 32];
+#pragma unroll
+    for (int cb = 0; cb < kD / 32; ++cb) o[cb] = mfma::zero16();
+    float top = kNone, sum = 0.f;
+
+    for (int t0 = begin; t0 < end; t0 += 32) {
+        const int kt = min(t0 + col, end - 1);                       // (rows past the share's end: its last one again, weight 0)
+        const size_t krow = row_in_pool(a.cache, page_of(a.cache, x.b, kt), x.g, kt);
+        f32x16 z = mfma::zero16();
+#pragma unroll
+        for (int s = 0; s < kD / 8; ++s) {
+            float k[4];
+            const int lo = 8 * s + 4 * half;
+            if constexpr (kCodes) {
+                e4m3_values(*(const uint32_t *)(a.cache.k + krow * kD + lo), scale_value(a.cache.k_scale[krow * (kD / kScaleBlock) + s / 4]), k);
+            } else if constexpr (kDtype == OBC_BF16) {
+                const u32x2 w = *(const u32x2 *)(a.cache.k + krow * (kD * 2) + lo * 2);
+                k[0] = __uint_as_float(w[0] << 16); k[1] = __uint_as_float(w[0] & 0xffff0000u);
+                k[2] = __uint_as_float(w[1] << 16); k[3] = __uint_as_float(w[1] & 0xffff0000u);
+            } else {
+                *(float4 *)k = *(const float4 *)(a.cache.k + krow * (kD * 4) + lo * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i], q[4 * s + i], z, 0, 0, 0);
+        }
+        float most = kNone;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int tok = t0 + 8 * (r / 4) + 4 * half + r % 4;
+            z[r] = tok < min(seen, end) ? z[r] * a.scale_log2 : -__builtin_inff();
+            most = fmaxf(most, z[r]);
+        }
+        const float now = fmaxf(top, mfma::halves_max(most));
+        const float shrink = __builtin_amdgcn_exp2f(top - now);
+        top = now;
+        sum *= shrink;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            z[r] = __builtin_amdgcn_exp2f(z[r] - now);
+            sum += z[r];
+        }
+#pragma unroll
+        for (int cb = 0; cb < kD / 32; ++cb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[cb][r] *= shrink;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int vt = min(t0 + 8 * (r / 4) + 4 * half + r % 4, end - 1);
+            const size_t vrow = row_in_pool(a.cache, page_of(a.cache, x.b, vt), x.g, vt);
+#pragma unroll
+            for (int cb = 0; cb < kD / 32; ++cb) {
+                float v;
+                const int ch = 32 * cb + col;
+                if constexpr (kCodes) {
+                    const uint32_t code = *(const uint8_t *)(a.cache.v + vrow * kD + ch);
+                    v = __builtin_amdgcn_cvt_f32_fp8((int)code, 0) * scale_value(a.cache.v_scale[vrow * (kD / kScaleBlock) + cb]);
+                } else if constexpr (kDtype == OBC_BF16) {
+                    v = bf16_bits_to_float(*(const uint16_t *)(a.cache.v + (vrow * kD + ch) * 2));
+                } else {
+                    v = *(const float *)(a.cache.v + (vrow * kD + ch) * 4);
+                }
+                o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[r], o[cb], 0, 0, 0);
+            }
+        }
+    }
+    sum = mfma::halves_sum(sum);
+    if (!exists) return;
+    if (plan.splits == 1) {
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        char *to = a.out + (((size_t)x.b * a.T + t) * a.Hq + h) * (kD * kSize);
+#pragma unroll
+        for (int cb = 0; cb < kD / 32; ++cb)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float y[4] = {o[cb][4 * j] * inv, o[cb][4 * j + 1] * inv, o[cb][4 * j + 2] * inv, o[cb][4 * j + 3] * inv};
+                store4<kDtype>(to + (32 * cb + 8 * j + 4 * half) * kSize, y);
+            }
+        return;
+    }
+    const size_t rec = ((size_t)split * a.B * a.Hkv + bg) * ((size_t)a.G * a.T) + row;
+    if (half == 0) part_ml[rec] = make_float2(top, sum);
+#pragma unroll
+    for (int cb = 0; cb < kD / 32; ++cb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *(float4 *)(part_o + rec * kD + 32 * cb + 8 * j + 4 * half) =
+                make_float4(o[cb][4 * j], o[cb][4 * j + 1], o[cb][4 * j + 2], o[cb][4 * j + 3]);
+}
+
+// Joins the shares of a row: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  One workgroup per row; 256 / (d / 4) shares at a time.
+template <int kD, int kDtype>
+__global__ __launch_bounds__(256) void attend_join(AttendArgs a, AttendPlan plan, const float2 *part_ml, const float *part_o) {
+    constexpr int kLanes = kD / 4, kSlots = 256 / kLanes, kSize = kDtype == OBC_BF16 ? 2 : 4;
+    __shared__ float4 sums[kSlots][kLanes];
+    __shared__ float2 ml[kSlots];
+    const int rows = a.G * a.T;
+    const int bg = blockIdx.x / rows, row = blockIdx.x % rows;
+    const Tile x = tile_of(a, bg, row / plan.tile_rows * plan.tile_rows, plan.tile_rows);
+    const int share = share_of(x.seen, plan.splits, plan.min_share);
+    const int shares = max((x.seen + share - 1) / share, 1);
+    const int slot = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+    float top = kNone, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = slot; s < shares; s += kSlots) {
+        const size_t rec = ((size_t)s * a.B * a.Hkv + bg) * rows + row;
+        const float2 m = part_ml[rec];
+        const float4 o = *(const float4 *)(part_o + rec * kD + 4 * c);
+        const float now = fmaxf(top, m.x), old = __builtin_amdgcn_exp2f(top - now), w = __builtin_amdgcn_exp2f(m.x - now);
+        top = now;
+        sum = sum * old + m.y * w;
+        acc.x = acc.x * old + o.x * w; acc.y = acc.y * old + o.y * w; acc.z = acc.z * old + o.z * w; acc.w = acc.w * old + o.w * w;
+    }
+    sums[slot][c] = acc;
+    if (c == 0) ml[slot] = make_float2(top, sum);
+    __syncthreads();
+    if (slot != 0) return;
+    for (int s = 1; s < kSlots; ++s) {
+        const float2 m = ml[s];
+        const float4 o = sums[s][c];
+        const float now = fmaxf(top, m.x), old = __builtin_amdgcn_exp2f(top - now), w = __builtin_amdgcn_exp2f(m.x - now);
+        top = now;
+        sum = sum * old + m.y * w;
+        acc.x = acc.x * old + o.x * w; acc.y = acc.y * old + o.y * w; acc.z = acc.z * old + o.z * w; acc.w = acc.w * old + o.w * w;
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const int t = row / a.G, h = x.g * a.G + row % a.G;
+    const float y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+    store4<kDtype>(a.out + ((((size_t)x.b * a.T + t) * a.Hq + h) * kD + 4 * c) * kSize, y);
+}
+
+template <typename F>
+hipError_t with_types(int d, int dtype, int cache_dtype, F &&f) {
+    const bool codes = cache_dtype == OBC_E4M3;
+    using std::integral_constant;
+    const auto by_codes = [&](auto dim, auto type) {
+        return codes ? f(dim, type, std::true_type()) : f(dim, type, std::false_type());
+    };
+    const auto by_type = [&](auto dim) {
+        return dtype == OBC_BF16 ? by_codes(dim, integral_constant<int, OBC_BF16>()) : by_codes(dim, integral_constant<int, OBC_F32>());
+    };
+    return d == 128 ? by_type(integral_constant<int, 128>()) : by_type(integral_constant<int, 64>());
+}
+
+size_t align_up(size_t x, size_t to) { return (x + to - 1) / to * to; }
+
+}  // namespace
+
+void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, int cache_dtype, AttendPlan *p) {
+    const long long rows = (long long)Hq / Hkv * T, heads = (long long)B * Hkv;
+    *p = {};
+    p->tile_rows = 32;
+    p->tiles = (int)((rows + 31) / 32);
+    p->min_share = 32;
+    // enough waves to fill the chip twice, shares of at least 128 tokens
+    const long long want = (2048 + heads * p->tiles - 1) / (heads * p->tiles);
+    p->splits = (int)std::max(1LL, std::min(want, (long long)(capacity + 127) / 128));
+    if (p->splits > 1) {
+        const size_t records = (size_t)p->splits * heads * rows;
+        p->part_ml = 0;
+        p->part_o = align_up(records * sizeof(float2), 256);
+        p->total = align_up(p->part_o + records * d * sizeof(float), 256);
+    }
+}
+
+hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, char *workspace, hipStream_t stream) {
+    return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
+        float2 *ml = (float2 *)(workspace + p.part_ml);
+        float *o = (float *)(workspace + p.part_o);
+        const long long units = (long long)p.tiles * p.splits * a.B * a.Hkv;
+        attend_plain<dim.value, type.value, codes.value><<<dim3((unsigned)((units + 3) / 4)), 256, 0, stream>>>(a, p, ml, o);
+        if (p.splits > 1)
+            attend_join<dim.value, type.value><<<dim3((unsigned)(a.B * a.Hkv * a.G * a.T)), 256, 0, stream>>>(a, p, ml, o);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace obc

@@ -1,0 +1,125 @@
+// The cache that kept and new rows live in, as the kernels see it, and its 8-bit number format.
+// Internal to the library.
+#pragma once
+
+#include "internal.h"
+
+namespace obc {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
+typedef float f32_pair __attribute__((ext_vector_type(2)));
+
+// Pages of `slots` = 2^shift rows per KV head; without a table sequence b is page b, which holds all of its rows.
+struct CacheView {
+    char *k, *v;
+    uint8_t *k_scale, *v_scale;
+    const int32_t *table;
+    int num_pages, pages_per_seq, page_size, shift, Hkv, capacity;   // shift: 31 without a table
+};
+
+// Device lengths: one per sequence, or one per (sequence, KV head).
+struct DeviceLens {
+    const int32_t *len;
+    int per_head;
+};
+__device__ __forceinline__ int device_len(const DeviceLens &l, int b, int g, int Hkv) {
+    return l.len[l.per_head ? b * Hkv + g : b];
+}
+
+// Row index inside the pool, in rows, of row `j` of KV head g: page * Hkv * slots + g * slots + slot.  64 bits: a pool may have more
+// than 2^31 elements.  Page numbers are device data that nobody has checked: outside the pool they are brought inside.
+__device__ __forceinline__ int page_of(const CacheView &c, int b, int j) {
+    const int p = c.table ? c.table[(size_t)b * c.pages_per_seq + (j >> c.shift)] : b;
+    return min(max(p, 0), c.num_pages - 1);
+}
+__device__ __forceinline__ size_t row_in_pool(const CacheView &c, int page, int g, int j) {
+    return ((size_t)page * c.Hkv + g) * c.page_size + (j & ((1u << c.shift) - 1));
+}
+
+// ---- e4m3 with one power of two per 32 channels ----------------------------------------------------------------------------
+// The stored byte is e + 127 with e the least integer for which absmax <= 448 * 2^e (absmax of the block's finite values), at
+// least -117, so that every value a code stands for is a normal fp32 (and bf16) number: 2^-9 * 2^-117 = 2^-126.  448 = 1.75 * 2^8.
+// Dividing by 2^e is exact and multiplying back is too, in bf16 as well (four significant bits): the only rounding is the one
+// to the code, and rows that are read back and stored again keep their values.
+constexpr int kScaleBlock = 32;
+constexpr uint32_t kLeastScale = 10;
+__device__ __forceinline__ uint32_t scale_byte(float absmax) {
+    const uint32_t u = __float_as_uint(absmax);
+    const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return (uint32_t)max(e, (int)kLeastScale);
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a < __builtin_inff() ? a : 0.f;
+}
+__device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) < __builtin_inff() ? x : __builtin_nanf(""); }
+// Four values (already divided by their power of two) to codes, rounded to nearest even.  An infinity or NaN becomes NaN.
+__device__ __forceinline__ uint32_t e4m3_codes(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(finite_or_nan(a), finite_or_nan(b), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(finite_or_nan(c), finite_or_nan(d), w, true);
+}
+__device__ __forceinline__ void e4m3_values(uint32_t codes, float scale, float (&x)[4]) {
+    const f32_pair lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    x[0] = lo[0] * scale; x[1] = lo[1] * scale; x[2] = hi[0] * scale; x[3] = hi[1] * scale;
+}
+// Four codes to four bf16 values, exactly.
+__device__ __forceinline__ u32x2 e4m3_bf16(uint32_t codes, float scale) {
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, scale, false);
+    const auto hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, scale, true);
+    return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+__device__ __forceinline__ uint32_t bf16_pair_of(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair){lo, hi}, bf16_pair));   // to nearest even
+}
+
+// ---- what the calls hand to the launchers ----------------------------------------------------------------------------------
+struct RowsView {            // rows of d contiguous elements at base + b * batch + t * token + h * head (bytes)
+    const char *base;
+    int64_t batch, token, head;
+};
+struct AppendArgs {
+    RowsView q, k, v;        // q.base may be null
+    CacheView cache;
+    char *q_out;             // [B,Hq,T,d]
+    DeviceLens lens, fresh;  // fresh.len null: T new rows everywhere
+    const int32_t *positions;
+    const float *inv_freq;
+    int pairs;               // 0: no rotation
+    float rot_scale;
+    int interleaved;
+    const void *q_norm, *k_norm;
+    float eps;
+    int B, T, Hq, d, dtype, cache_dtype;
+};
+struct ReadArgs {
+    CacheView cache;
+    const int32_t *keep;     // [B,Hkv,n] or null: rows 0 .. n-1
+    char *k_out, *v_out;
+    int B, n, d, dtype, cache_dtype;
+};
+struct AttendArgs {
+    const char *q;           // [B,Hq,T,d]
+    CacheView cache;
+    char *out;               // [B,T,Hq,d]
+    DeviceLens lens;
+    const int32_t *fresh;    // [B] or null
+    int B, T, Hq, Hkv, G, d, dtype, cache_dtype, causal;
+    float scale_log2;        // scale * log2(e)
+};
+// How a call is cut up: rows (query head, new token) of a KV head in tiles, tokens in `splits` shares.  Offsets into the workspace.
+struct AttendPlan {
+    int form;                // kernel
+    int tiles, tile_rows, splits, min_share;
+    size_t part_ml, part_o, total;
+};
+
+hipError_t launch_append(const AppendArgs &a, hipStream_t stream);
+hipError_t launch_cache_read(const ReadArgs &a, hipStream_t stream);
+void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, int cache_dtype, AttendPlan *p);
+hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, char *workspace, hipStream_t stream);
+
+}  // namespace obc

@@ -1,0 +1,223 @@
+// New rows into the cache (norm of each head, rotation by position, 8-bit codes) and rows out of it again.
+#include <type_traits>
+
+#include "cache.h"
+#include "wave_util.h"
+
+namespace obc {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kGroups = kThreads / 16;       // 16 lanes hold one row
+
+// d / 16 consecutive channels of a row, in fp32.
+template <int kN>
+__device__ __forceinline__ void load_row(const char *p, bool bf16, float (&x)[kN]) {
+    if (bf16) {
+        uint32_t w[kN / 2];
+        if constexpr (kN == 8) *(u32x4 *)w = *(const u32x4 *)p;
+        else *(u32x2 *)w = *(const u32x2 *)p;
+#pragma unroll
+        for (int i = 0; i < kN / 2; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; i += 4) *(float4 *)(x + i) = *(const float4 *)(p + 4 * i);
+    }
+}
+template <int kN>
+__device__ __forceinline__ void store_row(char *p, bool bf16, const float (&x)[kN]) {
+    if (bf16) {
+        uint32_t w[kN / 2];
+#pragma unroll
+        for (int i = 0; i < kN / 2; ++i) w[i] = bf16_pair_of(x[2 * i], x[2 * i + 1]);
+        if constexpr (kN == 8) *(u32x4 *)p = *(u32x4 *)w;
+        else *(u32x2 *)p = *(u32x2 *)w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; i += 4) *(float4 *)(p + 4 * i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    }
+}
+
+// One workgroup per new token (and per 16 * gridDim.y of its heads): a row of d channels lies in 16 lanes, so the sum of its
+// squares is four lane exchanges, and a lane keeps its channels' cosines and sines for all heads of the token.
+// The angle pos * f is reduced to a part of one turn in 64 bits: in fp32 the product alone would be off by 2^-24 of the angle,
+// 0.06 rad at a million tokens.
+template <int kD, int kDtype, bool kCodes>
+__global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
+    constexpr int kN = kD / 16;
+    constexpr bool kBf16 = kDtype == OBC_BF16;
+    constexpr int kSize = kBf16 ? 2 : 4;
+    __shared__ float2 turn[kD / 2];
+    const int b = blockIdx.x / a.T, t = blockIdx.x % a.T;
+    const int group = threadIdx.x / 16, c = threadIdx.x % 16;
+    const int Hkv = a.cache.Hkv, rows = a.Hq + 2 * Hkv;
+    const int step = kGroups * gridDim.y;
+    if (a.pairs) {
+        for (int i = threadIdx.x; i < a.pairs; i += kThreads) {
+            double turns = (double)a.positions[(size_t)b * a.T + t] * (double)a.inv_freq[i] * 0.15915494309189533577;
+            turns -= rint(turns);
+            float sn, cs;
+            sincospif(2.f * (float)turns, &sn, &cs);
+            turn[i] = make_float2(cs * a.rot_scale, sn * a.rot_scale);
+        }
+        __syncthreads();
+    }
+    // channels kN c .. kN c + kN - 1: their angles, and for pairs (i, i + pairs) the lane that holds the other ones
+    const int lo = kN * c;
+    const bool turned = lo < 2 * a.pairs;
+    const bool second = lo >= a.pairs;
+    const int partner = (threadIdx.x & 48) + (second ? c - a.pairs / kN : c + a.pairs / kN);
+    float cs[kN], sn[kN];
+    if (turned) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const float2 x = turn[a.interleaved ? (lo + i) / 2 : second ? lo + i - a.pairs : lo + i];
+            cs[i] = x.x;
+            sn[i] = (a.interleaved ? i % 2 == 0 : !second) ? -x.y : x.y;
+        }
+    }
+    for (int r = blockIdx.y * kGroups + group; r < rows; r += step) {
+        const int kind = r < a.Hq ? 0 : r < a.Hq + Hkv ? 1 : 2;           // q, k, v
+        const int h = kind == 0 ? r : kind == 1 ? r - a.Hq : r - a.Hq - Hkv;
+        const int n = a.fresh.len ? min(max(device_len(a.fresh, b, kind ? h : 0, Hkv), 0), a.T) : a.T;
+        char *q_to = kind == 0 ? a.q_out + (((size_t)b * a.Hq + h) * a.T + t) * (kD * kSize) + lo * kSize : nullptr;
+        float x[kN];
+        if (t >= n) {
+            if (kind == 0) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) x[i] = 0.f;
+                store_row<kN>(q_to, kBf16, x);
+            }
+            continue;
+        }
+        const RowsView &from = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+        load_row<kN>(from.base + b * from.batch + t * from.token + h * from.head + lo * kSize, kBf16, x);
+        const void *norm = kind == 0 ? a.q_norm : a.k_norm;
+        if (kind < 2 && norm) {
+            float w[kN], sum = 0.f;
+            load_row<kN>((const char *)norm + lo * kSize, kBf16, w);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) sum = fmaf(x[i], x[i], sum);
+            const float inv = 1.f / sqrtf(row16_reduce<SumOp>(sum) * (1.f / kD) + a.eps);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) x[i] = x[i] * inv * w[i];
+        }
+        if (kind < 2 && a.pairs) {
+            float y[kN];
+            if (a.interleaved) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) y[i] = x[i ^ 1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) y[i] = __shfl(x[i], partner);
+            }
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) x[i] = fmaf(x[i], cs[i], y[i] * sn[i]);
+            }
+        }
+        if (kind == 0) {
+            store_row<kN>(q_to, kBf16, x);
+            continue;
+        }
+        const int j = device_len(a.lens, b, h, Hkv) - n + t;
+        if (j < 0 || j >= a.cache.capacity) continue;                     // (a row that the cache has no room for)
+        const int page = a.cache.table ? a.cache.table[(size_t)b * a.cache.pages_per_seq + (j >> a.cache.shift)] : b;
+        if (page < 0 || page >= a.cache.num_pages) continue;
+        const size_t row = row_in_pool(a.cache, page, h, j);
+        if constexpr (!kCodes) {
+            store_row<kN>((kind == 1 ? a.cache.k : a.cache.v) + row * (kD * kSize) + lo * kSize, kBf16, x);
+        } else {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) top = fmaxf(top, finite_abs(x[i]));
+            top = fmaxf(top, dpp_pair<0xB1>(top));                        // the block's lanes: 4, or 8 of half as many channels
+            top = fmaxf(top, dpp_pair<0x4E>(top));
+            if constexpr (kN == 4) top = fmaxf(top, dpp_pair<0x141>(top));
+            const uint32_t byte = scale_byte(top);
+            const float inv = scale_inverse(byte);
+            uint32_t w[kN / 4];
+#pragma unroll
+            for (int i = 0; i < kN; i += 4) w[i / 4] = e4m3_codes(x[i] * inv, x[i + 1] * inv, x[i + 2] * inv, x[i + 3] * inv);
+            char *to = (kind == 1 ? a.cache.k : a.cache.v) + row * kD + lo;
+            if constexpr (kN == 8) *(u32x2 *)to = u32x2{w[0], w[1]};
+            else *(uint32_t *)to = w[0];
+            if (lo % kScaleBlock == 0) (kind == 1 ? a.cache.k_scale : a.cache.v_scale)[row * (kD / kScaleBlock) + lo / kScaleBlock] = (uint8_t)byte;
+        }
+    }
+}
+
+// Rows of the cache as bf16 or fp32, 8 channels per thread.  K and V in one launch.
+template <int kD, int kDtype, bool kCodes>
+__global__ __launch_bounds__(kThreads) void read_rows(ReadArgs a, size_t total) {
+    const size_t at = (size_t)blockIdx.x * kThreads + threadIdx.x;
+    if (at >= total) return;
+    constexpr int kPieces = kD / 8, kSize = kDtype == OBC_BF16 ? 2 : 4;
+    const size_t out_row = at / kPieces;                  // (b * Hkv + g) * n + j
+    const int lo = (int)(at % kPieces) * 8;
+    const size_t bg = out_row / a.n;
+    const int b = (int)(bg / a.cache.Hkv), g = (int)(bg % a.cache.Hkv);
+    int j = a.keep ? a.keep[out_row] : (int)(out_row % a.n);
+    char *to = (blockIdx.y == 0 ? a.k_out : a.v_out) + out_row * (kD * kSize) + lo * kSize;
+    const bool none = j < 0;
+    j = min(max(j, 0), a.cache.capacity - 1);
+    const size_t row = row_in_pool(a.cache, page_of(a.cache, b, j), g, j);
+    const char *pages = blockIdx.y == 0 ? a.cache.k : a.cache.v;
+    if constexpr (kCodes) {
+        const uint8_t *scales = blockIdx.y == 0 ? a.cache.k_scale : a.cache.v_scale;
+        u32x2 w = *(const u32x2 *)(pages + row * kD + lo);
+        const float s = none ? 0.f : scale_value(scales[row * (kD / kScaleBlock) + lo / kScaleBlock]);
+        if (none) w = u32x2{0, 0};
+        float x[4], y[4];
+        e4m3_values(w[0], s, x);
+        e4m3_values(w[1], s, y);
+        const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        store_row<8>(to, kDtype == OBC_BF16, z);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kSize / 2; ++i) {
+            const u32x4 x = none ? u32x4{0, 0, 0, 0} : *(const u32x4 *)(pages + row * (kD * kSize) + lo * kSize + 16 * i);
+            *(u32x4 *)(to + 16 * i) = x;
+        }
+    }
+}
+
+// Calls `f` with the kernel's compile-time choices.
+template <typename F>
+hipError_t with_types(int d, int dtype, int cache_dtype, F &&f) {
+    const bool codes = cache_dtype == OBC_E4M3;
+    using std::integral_constant;
+    const auto by_codes = [&](auto dim, auto type) {
+        return codes ? f(dim, type, std::true_type()) : f(dim, type, std::false_type());
+    };
+    const auto by_type = [&](auto dim) {
+        return dtype == OBC_BF16 ? by_codes(dim, integral_constant<int, OBC_BF16>()) : by_codes(dim, integral_constant<int, OBC_F32>());
+    };
+    return d == 128 ? by_type(integral_constant<int, 128>()) : by_type(integral_constant<int, 64>());
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendArgs &a, hipStream_t stream) {
+    const int rows = a.Hq + 2 * a.cache.Hkv;
+    const unsigned tokens = (unsigned)(a.B * a.T);
+    const unsigned groups = (rows + kGroups - 1) / kGroups;
+    const unsigned y = tokens < 1024 ? groups : 1;       // few tokens: every row a group of its own
+    return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
+        append_rows<dim.value, type.value, codes.value><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_cache_read(const ReadArgs &a, hipStream_t stream) {
+    const size_t total = (size_t)a.B * a.cache.Hkv * a.n * (a.d / 8);
+    return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
+        read_rows<dim.value, type.value, codes.value><<<dim3((unsigned)((total + kThreads - 1) / kThreads), 2), kThreads, 0, stream>>>(a, total);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace obc
