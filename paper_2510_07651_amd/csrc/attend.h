@@ -1,0 +1,63 @@
+// What the attention kernels share: tiles of rows, shares of the sequence, partial results.  Internal to the library.
+//
+// The rows (new token t, query head h of a KV head) of one KV head read the same keys and values, so they are taken together,
+// token by token: row r is token r / G of query head g G + r % G, and a tile of consecutive rows sees nearly the same tokens.
+#pragma once
+
+#include <type_traits>
+
+#include "cache.h"
+
+namespace obc {
+
+constexpr float kNone = -3.0e38f;      // running maximum of a row that has seen nothing: finite, so that differences stay numbers
+
+// Tokens the rows of new token t see of a KV head with `len` rows, `n` of them new.
+__device__ __forceinline__ int tokens_seen(int len, int n, int t, int causal) {
+    if (t >= n) return 0;
+    return causal ? max(len - n + t + 1, 0) : len;
+}
+
+struct Tile {            // rows r0 .. r0 + size - 1 of KV head g of sequence b
+    int b, g, r0, len, n, seen;      // seen: the most any of its rows sees
+};
+__device__ __forceinline__ Tile tile_of(const AttendArgs &a, int bg, int r0, int size) {
+    Tile x;
+    x.b = bg / a.Hkv;
+    x.g = bg % a.Hkv;
+    x.r0 = r0;
+    x.len = min(max(device_len(a.lens, x.b, x.g, a.Hkv), 0), a.cache.capacity);
+    x.n = a.fresh ? min(max(a.fresh[x.b], 0), a.T) : a.T;
+    const int first = r0 / a.G, last = min((r0 + size - 1) / a.G, x.n - 1);
+    x.seen = first <= last ? tokens_seen(x.len, x.n, last, a.causal) : 0;
+    return x;
+}
+// Tokens per share of a tile: the same in the kernels that leave partial sums and in the one that joins them.
+__device__ __forceinline__ int share_of(int seen, int splits, int min_share) {
+    const int even = (seen + splits - 1) / splits;
+    return max((even + min_share - 1) / min_share * min_share, min_share);
+}
+
+template <int kDtype>
+__device__ __forceinline__ void store4(char *p, const float (&x)[4]) {
+    if constexpr (kDtype == OBC_BF16) *(u32x2 *)p = u32x2{bf16_pair_of(x[0], x[1]), bf16_pair_of(x[2], x[3])};
+    else *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]);
+}
+
+// Calls `f` with a kernel's compile-time choices.
+template <typename F>
+hipError_t with_types(int d, int dtype, int cache_dtype, F &&f) {
+    const bool codes = cache_dtype == OBC_E4M3;
+    using std::integral_constant;
+    const auto by_codes = [&](auto dim, auto type) {
+        return codes ? f(dim, type, std::true_type()) : f(dim, type, std::false_type());
+    };
+    const auto by_type = [&](auto dim) {
+        return dtype == OBC_BF16 ? by_codes(dim, integral_constant<int, OBC_BF16>()) : by_codes(dim, integral_constant<int, OBC_F32>());
+    };
+    return d == 128 ? by_type(integral_constant<int, 128>()) : by_type(integral_constant<int, 64>());
+}
+
+hipError_t launch_attend_chunk(const AttendArgs &a, const AttendPlan &p, float2 *part_ml, float *part_o, hipStream_t stream);
+
+}  // namespace obc

@@ -1,10 +1,5 @@
 // Attention of new tokens over the cache: out = softmax(scale q k^T) v over the rows a token may see.
-//
-// The rows (new token t, query head h of a KV head) of one KV head read the same keys and values, so they are taken together,
-// token by token: row r is token r / G of query head g G + r % G, and a tile of consecutive rows sees nearly the same tokens.
-#include <type_traits>
-
-#include "cache.h"
+#include "attend.h"
 #include "mfma_util.h"
 #include "wave_util.h"
 
@@ -12,40 +7,6 @@ namespace obc {
 namespace {
 
 using mfma::f32x16;
-
-constexpr float kNone = -3.0e38f;      // running maximum of a row that has seen nothing: finite, so that differences stay numbers
-
-// Tokens the rows of new token t see of a KV head with `len` rows, `n` of them new.
-__device__ __forceinline__ int tokens_seen(int len, int n, int t, int causal) {
-    if (t >= n) return 0;
-    return causal ? max(len - n + t + 1, 0) : len;
-}
-
-struct Tile {            // rows r0 .. r0 + size - 1 of KV head g of sequence b
-    int b, g, r0, len, n, seen;      // seen: the most any of its rows sees
-};
-__device__ __forceinline__ Tile tile_of(const AttendArgs &a, int bg, int r0, int size) {
-    Tile x;
-    x.b = bg / a.Hkv;
-    x.g = bg % a.Hkv;
-    x.r0 = r0;
-    x.len = min(max(device_len(a.lens, x.b, x.g, a.Hkv), 0), a.cache.capacity);
-    x.n = a.fresh ? min(max(a.fresh[x.b], 0), a.T) : a.T;
-    const int first = r0 / a.G, last = min((r0 + size - 1) / a.G, x.n - 1);
-    x.seen = first <= last ? tokens_seen(x.len, x.n, last, a.causal) : 0;
-    return x;
-}
-// Tokens per share of a tile: the same in the kernels that leave partial sums and in the one that joins them.
-__device__ __forceinline__ int share_of(int seen, int splits, int min_share) {
-    const int even = (seen + splits - 1) / splits;
-    return max((even + min_share - 1) / min_share * min_share, min_share);
-}
-
-template <int kDtype>
-__device__ __forceinline__ void store4(char *p, const float (&x)[4]) {
-    if constexpr (kDtype == OBC_BF16) *(u32x2 *)p = u32x2{bf16_pair_of(x[0], x[1]), bf16_pair_of(x[2], x[3])};
-    else *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]);
-}
 
 // The general kernel, in fp32: one wave per (tile of 32 rows, share).  S^T = K Q^T and O^T = V^T P^T on the fp32 matrix cores: a
 // lane holds one row's column of both, so the softmax needs one exchange between the wave's halves and no shuffle of P:
@@ -209,19 +170,6 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, AttendPlan plan
     store4<kDtype>(a.out + ((((size_t)x.b * a.T + t) * a.Hq + h) * kD + 4 * c) * kSize, y);
 }
 
-template <typename F>
-hipError_t with_types(int d, int dtype, int cache_dtype, F &&f) {
-    const bool codes = cache_dtype == OBC_E4M3;
-    using std::integral_constant;
-    const auto by_codes = [&](auto dim, auto type) {
-        return codes ? f(dim, type, std::true_type()) : f(dim, type, std::false_type());
-    };
-    const auto by_type = [&](auto dim) {
-        return dtype == OBC_BF16 ? by_codes(dim, integral_constant<int, OBC_BF16>()) : by_codes(dim, integral_constant<int, OBC_F32>());
-    };
-    return d == 128 ? by_type(integral_constant<int, 128>()) : by_type(integral_constant<int, 64>());
-}
-
 size_t align_up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 
 }  // namespace
@@ -229,12 +177,22 @@ size_t align_up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, int cache_dtype, AttendPlan *p) {
     const long long rows = (long long)Hq / Hkv * T, heads = (long long)B * Hkv;
     *p = {};
-    p->tile_rows = 32;
-    p->tiles = (int)((rows + 31) / 32);
-    p->min_share = 32;
-    // enough waves to fill the chip twice, shares of at least 128 tokens
-    const long long want = (2048 + heads * p->tiles - 1) / (heads * p->tiles);
-    p->splits = (int)std::max(1LL, std::min(want, (long long)(capacity + 127) / 128));
+    long long want, least;              // workgroups (waves) that fill the chip, tokens of the shortest share
+    if (dtype == OBC_BF16 && cache_dtype == OBC_BF16 && rows > 32) {
+        p->form = kAttendChunk;
+        p->tile_rows = heads * ((rows + 255) / 256) >= 128 ? 256 : 128;
+        p->min_share = 32;
+        want = p->tile_rows == 256 ? 256 : 512;
+        least = 256;
+    } else {
+        p->form = kAttendPlain;
+        p->tile_rows = 32;
+        p->min_share = 32;
+        want = 2048;
+        least = 128;
+    }
+    p->tiles = (int)((rows + p->tile_rows - 1) / p->tile_rows);
+    p->splits = (int)std::max(1LL, std::min(want / (heads * p->tiles), (capacity + least - 1) / least));
     if (p->splits > 1) {
         const size_t records = (size_t)p->splits * heads * rows;
         p->part_ml = 0;
@@ -244,13 +202,21 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
 }
 
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, char *workspace, hipStream_t stream) {
-    return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
-        float2 *ml = (float2 *)(workspace + p.part_ml);
-        float *o = (float *)(workspace + p.part_o);
-        const long long units = (long long)p.tiles * p.splits * a.B * a.Hkv;
-        attend_plain<dim.value, type.value, codes.value><<<dim3((unsigned)((units + 3) / 4)), 256, 0, stream>>>(a, p, ml, o);
-        if (p.splits > 1)
-            attend_join<dim.value, type.value><<<dim3((unsigned)(a.B * a.Hkv * a.G * a.T)), 256, 0, stream>>>(a, p, ml, o);
+    float2 *ml = (float2 *)(workspace + p.part_ml);
+    float *o = (float *)(workspace + p.part_o);
+    hipError_t e = hipSuccess;
+    if (p.form == kAttendChunk) {
+        e = launch_attend_chunk(a, p, ml, o, stream);
+    } else {
+        e = with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
+            const long long units = (long long)p.tiles * p.splits * a.B * a.Hkv;
+            attend_plain<dim.value, type.value, codes.value><<<dim3((unsigned)((units + 3) / 4)), 256, 0, stream>>>(a, p, ml, o);
+            return hipGetLastError();
+        });
+    }
+    if (e != hipSuccess || p.splits == 1) return e;
+    return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto) {
+        attend_join<dim.value, type.value><<<dim3((unsigned)(a.B * a.Hkv * a.G * a.T)), 256, 0, stream>>>(a, p, ml, o);
         return hipGetLastError();
     });
 }

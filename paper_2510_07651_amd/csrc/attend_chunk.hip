@@ -1,0 +1,298 @@
+// Attention of a chunk of bf16 queries over the cache, on the bf16 matrix cores.
+#include "attend.h"
+#include "mfma_util.h"
+#include "wave_util.h"
+
+namespace obc {
+namespace {
+
+using mfma::bf16x8;
+using mfma::f32x16;
+using mfma::i16x4;
+
+constexpr int kThreads = 256;
+constexpr int kRing = 4;               // blocks of 32 tokens in LDS
+constexpr float kLazy = 8.f;           // log2 of how far a weight may grow past its reference before sums are rescaled
+
+template <int kD>
+struct Shape {
+    static constexpr int kRow = 2 * kD, kPieces = kD / 8, kBlock = 32 * kRow, kSlot = 2 * kBlock;     // a slot: K block, V block
+    static constexpr int kSteps = kD / 16, kCols = kD / 32;
+};
+
+// LDS blocks hold 32 rows of d bf16.  Row R keeps its 16-byte piece c at another slot, so that the reads meet no bank twice:
+// keys are read one piece of 16 consecutive rows at a time, values 64 contiguous bytes of 4 consecutive rows.
+template <int kD>
+__device__ __forceinline__ int key_slot(int R, int c) { return kD == 128 ? c ^ (R & 15) : c ^ ((R >> 1) & 7); }
+template <int kD>
+__device__ __forceinline__ int value_slot(int R, int c) { return kD == 128 ? (c + 4 * (R & 3)) & 15 : (c + 4 * ((R >> 1) & 1)) & 7; }
+template <int kD>
+__device__ __forceinline__ int value_piece(int R, int slot) { return kD == 128 ? (slot - 4 * (R & 3)) & 15 : (slot - 4 * ((R >> 1) & 1)) & 7; }
+
+typedef const __attribute__((address_space(4))) int32_t *table_ptr;    // read through scalar loads
+
+// Brings blocks of 32 rows of K and V into LDS.  Every wave brings 8 rows of each.
+template <int kD, bool kCodes>
+struct Loader;
+
+// bf16 rows go to LDS directly.  8 consecutive rows lie in one page where pages hold at least 8, and then the page is looked up by
+// a scalar load, once for the wave.
+template <int kD>
+struct Loader<kD, false> {
+    using S = Shape<kD>;
+    static constexpr int kRowsPer = 1024 / S::kRow, kParts = 8 / kRowsPer, kInFlight = 2 * kParts;   // transfers of a wave per block
+    const CacheView &c;
+    int b, g, end, wave, lane;
+    bool by_page;
+    uint32_t off_k[kParts], off_v[kParts];
+    uint32_t lds;
+
+    __device__ Loader(const CacheView &cache, const Tile &x, int end_, int wave_, int lane_, uint32_t lds_)
+        : c(cache), b(x.b), g(x.g), end(end_), wave(wave_), lane(lane_), by_page(cache.page_size >= 8), lds(lds_) {
+#pragma unroll
+        for (int n = 0; n < kParts; ++n) {
+            const int R = wave * 8 + n * kRowsPer + lane / S::kPieces, slot = lane % S::kPieces;
+            const int row = n * kRowsPer + lane / S::kPieces;
+            off_k[n] = row * S::kRow + key_slot<kD>(R, slot) * 16;
+            off_v[n] = row * S::kRow + value_piece<kD>(R, slot) * 16;
+        }
+    }
+    __device__ void issue(int t0, int slot) const {
+        const int t = t0 + wave * 8;
+        const uint32_t to = lds + slot * S::kSlot + wave * 8 * S::kRow;
+        if (by_page && t + 7 < end) {
+            int page = b;
+            if (c.table) page = ((table_ptr)(uintptr_t)(c.table + (size_t)b * c.pages_per_seq))[t >> c.shift];
+            page = min(max(page, 0), c.num_pages - 1);
+            const size_t at = row_in_pool(c, page, g, t) * S::kRow;
+#pragma unroll
+            for (int n = 0; n < kParts; ++n) mfma::dma16_based<false>(c.k + at, off_k[n], to + n * 1024);
+#pragma unroll
+            for (int n = 0; n < kParts; ++n) mfma::dma16_based<false>(c.v + at, off_v[n], to + S::kBlock + n * 1024);
+            return;
+        }
+#pragma unroll
+        for (int n = 0; n < kParts; ++n) {
+            const int row = n * kRowsPer + lane / S::kPieces;
+            const int j = min(t + row, end - 1);                        // (rows past the end: the last one again)
+            const size_t at = row_in_pool(c, page_of(c, b, j), g, j) * S::kRow;
+            mfma::dma16<false>(c.k + at + (off_k[n] - row * S::kRow), to + n * 1024);
+            mfma::dma16<false>(c.v + at + (off_v[n] - row * S::kRow), to + S::kBlock + n * 1024);
+        }
+    }
+};
+
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Workgroup of four waves, 32 kSets rows each, against a share of the sequence in blocks of 32 tokens.
+template <int kD, int kSets, bool kCodes>
+__global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
+    using S = Shape<kD>;
+    __shared__ __attribute__((aligned(1024))) char smem[kRing * S::kSlot];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+
+    // Which tile: workgroups go to the eight dies in turn; those of one KV head stay on as few as there are heads for, so that they
+    // find its rows in that die's L2.  Late tiles, which see most, first.
+    const int heads = a.B * a.Hkv, die = blockIdx.x & 7, classes = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
+    const int per_head = plan.tiles * plan.splits, line = (per_head + 8 / classes - 1) / (8 / classes);
+    const int at = (int)(blockIdx.x >> 3), place = die / classes + 8 / classes * (at % line);
+    const int bg = die % classes + classes * (at / line);
+    if (place >= per_head) return;
+    const int tile = plan.tiles - 1 - place / plan.splits, split = place % plan.splits;
+
+    const Tile x = tile_of(a, bg, tile * plan.tile_rows, plan.tile_rows);
+    const int share = share_of(x.seen, plan.splits, plan.min_share);
+    const int begin = split * share, end = min(begin + share, x.seen), blocks = (end - begin + 31) / 32;
+    if (blocks <= 0 && split > 0) return;
+
+    int row[kSets], seen[kSets], full[kSets];      // full: tokens that every row of the set that counts sees
+    bf16x8 q[kSets][S::kSteps];
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+        const int r0 = x.r0 + (wave * kSets + s) * 32;
+        row[s] = r0 + col;
+        const int t = row[s] / a.G, h = x.g * a.G + row[s] % a.G;
+        const bool exists = t < a.T;
+        seen[s] = exists ? min(tokens_seen(x.len, x.n, t, a.causal), end) : 0;
+        full[s] = r0 / a.G < x.n ? min(tokens_seen(x.len, x.n, r0 / a.G, a.causal), end) : 0;
+        const char *p = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * S::kRow + half * 16;
+#pragma unroll
+        for (int k = 0; k < S::kSteps; ++k) q[s][k] = *(const bf16x8 *)(p + 32 * k);
+    }
+    f32x16 o[kSets][S::kCols], z[kSets];
+    float top[kSets], sum[kSets];
+    union Weights { uint32_t u[8]; bf16x8 v[2]; } w[kSets];
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+        top[s] = kNone;
+        sum[s] = 0.f;
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) o[s][c] = mfma::zero16();
+#pragma unroll
+        for (int k = 0; k < S::kSteps; ++k) mfma::settle(q[s][k]);
+    }
+
+    if (blocks > 0) {
+        const uint32_t lds = mfma::lds_offset_of(smem);
+        const Loader<kD, kCodes> load(a.cache, x, end, wave, lane, lds);
+        int k_off[S::kSteps], v_off[S::kCols];
+#pragma unroll
+        for (int k = 0; k < S::kSteps; ++k) k_off[k] = col * S::kRow + key_slot<kD>(col, 2 * k + half) * 16;
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) {
+            const int i = lane & 15, sub = (lane >> 4) & 1, R = 4 * half + (i >> 2);
+            v_off[c] = S::kBlock + R * S::kRow + value_slot<kD>(R, c * 4 + sub * 2 + ((i & 3) >> 1)) * 16 + (i & 1) * 8;
+        }
+        bf16x8 kb[S::kSteps], vb[S::kCols][2];
+        const auto read_keys = [&](int i) {
+            const char *p = smem + (i % kRing) * S::kSlot;
+#pragma unroll
+            for (int k = 0; k < S::kSteps; ++k) kb[k] = mfma::lds_read16(p + k_off[k]);
+        };
+        const auto read_values = [&](int i) {
+            const char *p = smem + (i % kRing) * S::kSlot;
+#pragma unroll
+            for (int c = 0; c < S::kCols; ++c)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    union { bf16x8 v; i16x4 h[2]; } u;
+                    typedef __attribute__((address_space(3))) i16x4 *lds4;
+                    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + v_off[c] + 16 * k * S::kRow));
+                    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + v_off[c] + (16 * k + 8) * S::kRow));
+                    vb[c][k] = u.v;
+                }
+        };
+        const auto logits = [&](int s) {
+            z[s] = mfma::zero16();
+#pragma unroll
+            for (int k = 0; k < S::kSteps; ++k) z[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[k], q[s][k], z[s], 0, 0, 0);
+        };
+        const auto outputs = [&](int s, int from, int to) {
+#pragma unroll
+            for (int j = from; j < to; ++j) o[s][j / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j / 2][j % 2], w[s].v[j % 2], o[s][j / 2], 0, 0, 0);
+        };
+        // Hides what a row does not see and moves its reference if a logit has outgrown it.
+        const auto reference = [&](int s, int i) {
+            const int t0 = begin + 32 * i;
+            if (t0 + 32 > full[s]) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[s][r] = t0 + 8 * (r / 4) + 4 * half + r % 4 < seen[s] ? z[s][r] : -__builtin_inff();
+            }
+            float most = mfma::max3(z[s][0], z[s][1], z[s][2]);
+#pragma unroll
+            for (int r = 3; r < 15; r += 2) most = mfma::max3(most, z[s][r], z[s][r + 1]);
+            most = mfma::halves_max(fmaxf(most, z[s][15])) * a.scale_log2;
+            if (__any(most > top[s] + kLazy)) {
+                const float now = fmaxf(top[s], most), shrink = __builtin_amdgcn_exp2f(top[s] - now);
+                top[s] = now;
+                sum[s] *= shrink;
+#pragma unroll
+                for (int c = 0; c < S::kCols; ++c)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[s][c][r] *= shrink;
+            }
+        };
+        const auto weights = [&](int s) {
+            const mfma::bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(z[s][r], a.scale_log2, -top[s]));
+                const float f = __builtin_amdgcn_exp2f(fmaf(z[s][r + 1], a.scale_log2, -top[s]));
+                w[s].u[r / 2] = mfma::pack_bf16(e, f);
+                sum[s] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2, w[s].u[r / 2]), one, sum[s], false);
+            }
+        };
+
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < blocks) load.issue(begin + 32 * i, i);
+        mfma::wait_async_loads();
+        barrier();
+        read_keys(0);
+        read_values(0);
+#pragma unroll
+        for (int s = 0; s < kSets; ++s) logits(s);
+        if constexpr (kSets == 2) {
+            reference(0, 0);
+            weights(0);
+        }
+        const auto step = [&](int i, auto last) {
+            if constexpr (!last.value) {
+                if (i + 2 < blocks) mfma::wait_async_loads_keep<Loader<kD, kCodes>::kInFlight>();
+                else mfma::wait_async_loads();
+                barrier();
+                if (i + 3 < blocks) load.issue(begin + 32 * (i + 3), (i + 3) % kRing);
+            }
+            if constexpr (kSets == 2) {
+                outputs(0, 0, S::kCols);
+                reference(1, i);
+                if constexpr (!last.value) read_keys(i + 1);
+                outputs(0, S::kCols, 2 * S::kCols);
+                if constexpr (!last.value) logits(0);
+                weights(1);
+                outputs(1, 0, S::kCols);
+                if constexpr (!last.value) reference(0, i + 1);
+                outputs(1, S::kCols, 2 * S::kCols);
+                if constexpr (!last.value) {
+                    read_values(i + 1);
+                    logits(1);
+                    weights(0);
+                }
+            } else {
+                reference(0, i);
+                weights(0);
+                if constexpr (!last.value) {
+                    read_keys(i + 1);
+                    logits(0);
+                }
+                outputs(0, 0, 2 * S::kCols);
+                if constexpr (!last.value) read_values(i + 1);
+            }
+        };
+        for (int i = 0; i + 1 < blocks; ++i) step(i, std::false_type());
+        step(blocks - 1, std::true_type());
+    }
+
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+        // (rows behind the chunk's end share a set with rows that see something: what they have summed up is dropped here)
+        const bool sees = seen[s] > 0;
+        const float both = mfma::halves_sum(sum[s]), total = sees ? both : 0.f;
+        const int t = row[s] / a.G, h = x.g * a.G + row[s] % a.G;
+        if (t >= a.T) continue;
+        const bool whole = plan.splits == 1;
+        const float by = !sees ? 0.f : whole ? 1.f / total : 1.f;
+        const size_t rec = ((size_t)split * heads + bg) * ((size_t)a.G * a.T) + row[s];
+        if (!whole && half == 0) part_ml[rec] = make_float2(sees ? top[s] : kNone, total);
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int ch = 32 * c + 8 * j + 4 * half;
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = sees ? o[s][c][4 * j + i] * by : 0.f;
+                if (whole) store4<OBC_BF16>(a.out + ((((size_t)x.b * a.T + t) * a.Hq + h) * kD + ch) * 2, y);
+                else store4<OBC_F32>((char *)(part_o + rec * kD + ch), y);
+            }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_attend_chunk(const AttendArgs &a, const AttendPlan &p, float2 *part_ml, float *part_o, hipStream_t stream) {
+    const int heads = a.B * a.Hkv, classes = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
+    const long long per_head = (long long)p.tiles * p.splits, line = (per_head + 8 / classes - 1) / (8 / classes);
+    const dim3 grid((unsigned)(8 * line * (heads / classes)));
+    const auto go = [&](auto dim, auto sets) {
+        attend_chunk<dim.value, sets.value, false><<<grid, kThreads, 0, stream>>>(a, p, part_ml, part_o);
+        return hipGetLastError();
+    };
+    using std::integral_constant;
+    const auto by_sets = [&](auto dim) {
+        return p.tile_rows == 256 ? go(dim, integral_constant<int, 2>()) : go(dim, integral_constant<int, 1>());
+    };
+    return a.d == 128 ? by_sets(integral_constant<int, 128>()) : by_sets(integral_constant<int, 64>());
+}
+
+}  // namespace obc
