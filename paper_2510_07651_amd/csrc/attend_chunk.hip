@@ -129,7 +129,11 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
 #pragma unroll
         for (int c = 0; c < S::kCols; ++c) o[s][c] = mfma::zero16();
 #pragma unroll
-        for (int k = 0; k < S::kSteps; ++k) mfma::settle(q[s][k]);
+        for (int k = 0; k < S::kSteps; ++k) {
+            // (waits for the load here; queries of two sets are for the matrix cores alone and lie in the accumulator file)
+            if constexpr (kSets == 2) asm volatile("" : "+a"(q[s][k]));
+            else mfma::settle(q[s][k]);
+        }
     }
 
     if (blocks > 0) {
@@ -167,39 +171,88 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
 #pragma unroll
             for (int k = 0; k < S::kSteps; ++k) z[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[k], q[s][k], z[s], 0, 0, 0);
         };
-        const auto outputs = [&](int s, int from, int to) {
-#pragma unroll
-            for (int j = from; j < to; ++j) o[s][j / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j / 2][j % 2], w[s].v[j % 2], o[s][j / 2], 0, 0, 0);
+        const auto output = [&](int s, int j) {
+            o[s][j / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j / 2][j % 2], w[s].v[j % 2], o[s][j / 2], 0, 0, 0);
         };
-        // Hides what a row does not see and moves its reference if a logit has outgrown it.
-        const auto reference = [&](int s, int i) {
+        // Hides what a row does not see.
+        const auto hide = [&](int s, int i) {
             const int t0 = begin + 32 * i;
             if (t0 + 32 > full[s]) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) z[s][r] = t0 + 8 * (r / 4) + 4 * half + r % 4 < seen[s] ? z[s][r] : -__builtin_inff();
             }
+        };
+        const auto largest = [&](int s) {
             float most = mfma::max3(z[s][0], z[s][1], z[s][2]);
 #pragma unroll
             for (int r = 3; r < 15; r += 2) most = mfma::max3(most, z[s][r], z[s][r + 1]);
-            most = mfma::halves_max(fmaxf(most, z[s][15])) * a.scale_log2;
+            return mfma::halves_max(fmaxf(most, z[s][15])) * a.scale_log2;
+        };
+        // Moves a row's reference if a logit has outgrown it.  (The sums stay in the accumulator file: without the ties the compiler
+        // carries a copy of them around the loop for this branch, 64 moves per block.)
+        const auto refer = [&](int s, float most) {
             if (__any(most > top[s] + kLazy)) {
                 const float now = fmaxf(top[s], most), shrink = __builtin_amdgcn_exp2f(top[s] - now);
                 top[s] = now;
                 sum[s] *= shrink;
 #pragma unroll
-                for (int c = 0; c < S::kCols; ++c)
+                for (int c = 0; c < S::kCols; ++c) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[s][c][r] *= shrink;
+                    
+                }
             }
         };
-        const auto weights = [&](int s) {
-            const mfma::bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+        // Weights of the set's pairs from .. to - 1 of eight: two tokens each.
+        const mfma::bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+        const auto weigh = [&](int s, int from, int to) {
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(z[s][r], a.scale_log2, -top[s]));
-                const float f = __builtin_amdgcn_exp2f(fmaf(z[s][r + 1], a.scale_log2, -top[s]));
-                w[s].u[r / 2] = mfma::pack_bf16(e, f);
-                sum[s] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2, w[s].u[r / 2]), one, sum[s], false);
+            for (int j = from; j < to; ++j) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(z[s][2 * j], a.scale_log2, -top[s]));
+                const float f = __builtin_amdgcn_exp2f(fmaf(z[s][2 * j + 1], a.scale_log2, -top[s]));
+                w[s].u[j] = mfma::pack_bf16(e, f);
+                sum[s] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2, w[s].u[j]), one, sum[s], false);
+            }
+        };
+        // Half a step with two sets: the matrix cores add set `s`'s weights times this block's values and form its logits of the next
+        // block, while the vector ALUs turn the other set's logits into weights.  One matrix op and a slice of vector work per slot.
+        const auto half_step = [&](auto set, int block_other, int next, auto last) {
+            constexpr int s = set.value, u = 1 - s, kOut = 2 * S::kCols;
+            const auto slot_end = [] { __builtin_amdgcn_sched_barrier(0); };
+            output(s, 0);
+            if constexpr (s == 0 && !last.value) read_keys(next);
+            slot_end();
+            output(s, 1);
+            slot_end();
+            constexpr bool kNoOther = s == 1 && last.value;          // (the last block has nobody's next logits)
+            float most = 0.f;
+            if constexpr (!kNoOther) hide(u, block_other);
+            output(s, 2);
+            if constexpr (!kNoOther) most = largest(u);
+            output(s, 3);
+            if constexpr (!kNoOther) refer(u, most);
+            slot_end();
+            constexpr int kLeft = kOut - 4;
+            if constexpr (kLeft > 0) {
+#pragma unroll
+                for (int j = 0; j < kLeft; ++j) {
+                    output(s, 4 + j);
+                    if constexpr (!kNoOther) weigh(u, j / 2, (j + 1) / 2);
+                    slot_end();
+                }
+            }
+            if constexpr (!last.value) {
+                if constexpr (s == 1) read_values(next);
+                z[s] = mfma::zero16();
+#pragma unroll
+                for (int k = 0; k < S::kSteps; ++k) {
+                    z[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[k], q[s][k], z[s], 0, 0, 0);
+                    constexpr int kDone = kLeft / 2;
+                    weigh(u, kDone + k * (8 - kDone) / S::kSteps, kDone + (k + 1) * (8 - kDone) / S::kSteps);
+                    slot_end();
+                }
+            } else if constexpr (!kNoOther) {
+                weigh(u, kLeft / 2, 8);
             }
         };
 
@@ -213,8 +266,9 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
 #pragma unroll
         for (int s = 0; s < kSets; ++s) logits(s);
         if constexpr (kSets == 2) {
-            reference(0, 0);
-            weights(0);
+            hide(0, 0);
+            refer(0, largest(0));
+            weigh(0, 0, 8);
         }
         const auto step = [&](int i, auto last) {
             if constexpr (!last.value) {
@@ -224,28 +278,18 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
                 if (i + 3 < blocks) load.issue(begin + 32 * (i + 3), (i + 3) % kRing);
             }
             if constexpr (kSets == 2) {
-                outputs(0, 0, S::kCols);
-                reference(1, i);
-                if constexpr (!last.value) read_keys(i + 1);
-                outputs(0, S::kCols, 2 * S::kCols);
-                if constexpr (!last.value) logits(0);
-                weights(1);
-                outputs(1, 0, S::kCols);
-                if constexpr (!last.value) reference(0, i + 1);
-                outputs(1, S::kCols, 2 * S::kCols);
-                if constexpr (!last.value) {
-                    read_values(i + 1);
-                    logits(1);
-                    weights(0);
-                }
+                half_step(std::integral_constant<int, 0>(), i, i + 1, last);
+                half_step(std::integral_constant<int, 1>(), i + 1, i + 1, last);
             } else {
-                reference(0, i);
-                weights(0);
+                hide(0, i);
+                refer(0, largest(0));
+                weigh(0, 0, 8);
                 if constexpr (!last.value) {
                     read_keys(i + 1);
                     logits(0);
                 }
-                outputs(0, 0, 2 * S::kCols);
+#pragma unroll
+                for (int j = 0; j < 2 * S::kCols; ++j) output(0, j);
                 if constexpr (!last.value) read_values(i + 1);
             }
         };
