@@ -58,6 +58,7 @@ hipError_t with_types(int d, int dtype, int cache_dtype, F &&f) {
     return d == 128 ? by_type(integral_constant<int, 128>()) : by_type(integral_constant<int, 64>());
 }
 
+hipError_t launch_attend_token(const AttendArgs &a, const AttendPlan &p, float2 *part_ml, float *part_o, hipStream_t stream);
 hipError_t launch_attend_chunk(const AttendArgs &a, const AttendPlan &p, float2 *part_ml, float *part_o, hipStream_t stream);
 
 }  // namespace obc

@@ -178,7 +178,13 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
     const long long rows = (long long)Hq / Hkv * T, heads = (long long)B * Hkv;
     *p = {};
     long long want, least;              // workgroups (waves) that fill the chip, tokens of the shortest share
-    if (dtype == OBC_BF16 && cache_dtype == OBC_BF16 && rows > 32) {
+    if (dtype == OBC_BF16 && rows <= 32) {
+        p->form = kAttendToken;
+        p->tile_rows = rows <= 16 ? 16 : 32;
+        p->min_share = 128;
+        want = 1024;
+        least = 128;
+    } else if (dtype == OBC_BF16 && cache_dtype == OBC_BF16) {
         p->form = kAttendChunk;
         p->tile_rows = heads * ((rows + 255) / 256) >= 128 ? 256 : 128;
         p->min_share = 32;
@@ -207,6 +213,8 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, char *workspa
     hipError_t e = hipSuccess;
     if (p.form == kAttendChunk) {
         e = launch_attend_chunk(a, p, ml, o, stream);
+    } else if (p.form == kAttendToken) {
+        e = launch_attend_token(a, p, ml, o, stream);
     } else {
         e = with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
             const long long units = (long long)p.tiles * p.splits * a.B * a.Hkv;

@@ -20,7 +20,7 @@ int check_cache(const obc_cache_t *c, CacheView *view) {
     if (c->d != 64 && c->d != 128) return OBC_EUNSUPPORTED;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->page_table, 4)) return OBC_EINVAL;
     if (c->dtype == OBC_E4M3) {
-        if (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return OBC_EINVAL;
+        if (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)) return OBC_EINVAL;
     } else if (c->k_scale || c->v_scale) {
         return OBC_EINVAL;
     }
