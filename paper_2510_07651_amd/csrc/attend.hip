@@ -184,7 +184,7 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
         p->min_share = 128;
         want = 1024;
         least = 128;
-    } else if (dtype == OBC_BF16 && cache_dtype == OBC_BF16) {
+    } else if (dtype == OBC_BF16) {
         p->form = kAttendChunk;
         p->tile_rows = heads * ((rows + 255) / 256) >= 128 ? 256 : 128;
         p->min_share = 32;

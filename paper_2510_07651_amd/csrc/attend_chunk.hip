@@ -31,7 +31,11 @@ __device__ __forceinline__ int value_piece(int R, int slot) { return kD == 128 ?
 
 typedef const __attribute__((address_space(4))) int32_t *table_ptr;    // read through scalar loads
 
-// Brings blocks of 32 rows of K and V into LDS.  Every wave brings 8 rows of each.
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Brings blocks of 32 rows of K and V into LDS, block i of the share to slot i % kRing.  start(): block 0 is there after the next
+// barrier, and what follows is under way; turn(i), by all waves: block i + 1 is there and block i - 1 may be overwritten; slice(0, i),
+// slice(1, i): what is left to do of step i, between its first matrix ops.
 template <int kD, bool kCodes>
 struct Loader;
 
@@ -42,13 +46,14 @@ struct Loader<kD, false> {
     using S = Shape<kD>;
     static constexpr int kRowsPer = 1024 / S::kRow, kParts = 8 / kRowsPer, kInFlight = 2 * kParts;   // transfers of a wave per block
     const CacheView &c;
-    int b, g, end, wave, lane;
+    int b, g, begin, end, blocks, wave, lane;
     bool by_page;
     uint32_t off_k[kParts], off_v[kParts];
     uint32_t lds;
 
-    __device__ Loader(const CacheView &cache, const Tile &x, int end_, int wave_, int lane_, uint32_t lds_)
-        : c(cache), b(x.b), g(x.g), end(end_), wave(wave_), lane(lane_), by_page(cache.page_size >= 8), lds(lds_) {
+    __device__ Loader(const CacheView &cache, const Tile &x, int begin_, int end_, int wave_, int lane_, char *smem)
+        : c(cache), b(x.b), g(x.g), begin(begin_), end(end_), blocks((end_ - begin_ + 31) / 32), wave(wave_), lane(lane_),
+          by_page(!cache.table || cache.page_size >= 8), lds(mfma::lds_offset_of(smem)) {
 #pragma unroll
         for (int n = 0; n < kParts; ++n) {
             const int R = wave * 8 + n * kRowsPer + lane / S::kPieces, slot = lane % S::kPieces;
@@ -57,9 +62,22 @@ struct Loader<kD, false> {
             off_v[n] = row * S::kRow + value_piece<kD>(R, slot) * 16;
         }
     }
-    __device__ void issue(int t0, int slot) const {
-        const int t = t0 + wave * 8;
-        const uint32_t to = lds + slot * S::kSlot + wave * 8 * S::kRow;
+    __device__ void start() const {
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i)
+            if (i < blocks) issue(i);
+        mfma::wait_async_loads();
+    }
+    __device__ void turn(int i) const {
+        if (i + 2 < blocks) mfma::wait_async_loads_keep<kInFlight>();
+        else mfma::wait_async_loads();
+        barrier();
+        if (i + 3 < blocks) issue(i + 3);
+    }
+    __device__ void slice(int, int) const {}
+    __device__ void issue(int i) const {
+        const int t = begin + 32 * i + wave * 8;
+        const uint32_t to = lds + i % kRing * S::kSlot + wave * 8 * S::kRow;
         if (by_page && t + 7 < end) {
             int page = b;
             if (c.table) page = ((table_ptr)(uintptr_t)(c.table + (size_t)b * c.pages_per_seq))[t >> c.shift];
@@ -82,7 +100,65 @@ struct Loader<kD, false> {
     }
 };
 
-__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// 8-bit rows pass through registers: fetched a block ahead of when they are written to LDS as bf16, exactly (16 codes per thread
+// and tensor; with d = 64 half of the threads bring the keys, half the values).
+template <int kD>
+struct Loader<kD, true> {
+    using S = Shape<kD>;
+    static constexpr int kPerRow = kD / 16, kRows = 64 / kPerRow, kTensors = kD == 128 ? 2 : 1, kScales = kD / kScaleBlock;
+    const CacheView &c;
+    int b, g, begin, end, first, lane;        // first: the wave's first row of a block
+    bool by_page, values;
+    char *smem;
+    u32x4 x[kTensors];
+    uint32_t scale[kTensors];
+
+    __device__ Loader(const CacheView &cache, const Tile &tile, int begin_, int end_, int wave, int lane_, char *smem_)
+        : c(cache), b(tile.b), g(tile.g), begin(begin_), end(end_), first(kTensors == 2 ? wave * kRows : wave % 2 * kRows), lane(lane_),
+          by_page(!cache.table || cache.page_size >= kRows), values(kTensors == 1 && wave >= 2), smem(smem_) {}
+    __device__ void start() {
+        fetch(0);
+        slice(0, -2);
+        slice(1, -2);
+        slice(0, -1);
+        slice(1, -1);
+    }
+    __device__ void turn(int) const { barrier(); }
+    __device__ void slice(int n, int i) {
+        if (n < kTensors) stage(n, (i + 2) % kRing);
+        if (n == 1) fetch(i + 3);
+    }
+    __device__ void fetch(int i) {            // (blocks past the end: its last row)
+        const int t = begin + 32 * i + first, piece = lane % kPerRow;
+        size_t row;
+        if (by_page && t + kRows <= end) {
+            int page = b;
+            if (c.table) page = ((table_ptr)(uintptr_t)(c.table + (size_t)b * c.pages_per_seq))[t >> c.shift];
+            row = row_in_pool(c, min(max(page, 0), c.num_pages - 1), g, t) + lane / kPerRow;
+        } else {
+            const int j = min(t + lane / kPerRow, end - 1);
+            row = row_in_pool(c, page_of(c, b, j), g, j);
+        }
+#pragma unroll
+        for (int n = 0; n < kTensors; ++n) {
+            const bool v = kTensors == 2 ? n == 1 : values;
+            x[n] = *(const u32x4 *)((v ? c.v : c.k) + row * kD + piece * 16);
+            scale[n] = (v ? c.v_scale : c.k_scale)[row * kScales + piece / 2];
+        }
+    }
+    __device__ void stage(int n, int slot) const {
+        const bool v = kTensors == 2 ? n == 1 : values;
+        const int R = first + lane / kPerRow, piece = lane % kPerRow;
+        const float by = scale_value(scale[n]);
+        char *to = smem + slot * S::kSlot + (v ? S::kBlock : 0) + R * S::kRow;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u32x2 lo = e4m3_bf16(x[n][2 * h], by), hi = e4m3_bf16(x[n][2 * h + 1], by);
+            const int at = v ? value_slot<kD>(R, 2 * piece + h) : key_slot<kD>(R, 2 * piece + h);
+            *(u32x4 *)(to + at * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        }
+    }
+};
 
 // Workgroup of four waves, 32 kSets rows each, against a share of the sequence in blocks of 32 tokens.
 template <int kD, int kSets, bool kCodes>
@@ -137,8 +213,7 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
     }
 
     if (blocks > 0) {
-        const uint32_t lds = mfma::lds_offset_of(smem);
-        const Loader<kD, kCodes> load(a.cache, x, end, wave, lane, lds);
+        Loader<kD, kCodes> load(a.cache, x, begin, end, wave, lane, smem);
         int k_off[S::kSteps], v_off[S::kCols];
 #pragma unroll
         for (int k = 0; k < S::kSteps; ++k) k_off[k] = col * S::kRow + key_slot<kD>(col, 2 * k + half) * 16;
@@ -221,8 +296,10 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
             const auto slot_end = [] { __builtin_amdgcn_sched_barrier(0); };
             output(s, 0);
             if constexpr (s == 0 && !last.value) read_keys(next);
+            if constexpr (s == 0 && !last.value) load.slice(0, block_other);
             slot_end();
             output(s, 1);
+            if constexpr (s == 0 && !last.value) load.slice(1, block_other);
             slot_end();
             constexpr bool kNoOther = s == 1 && last.value;          // (the last block has nobody's next logits)
             float most = 0.f;
@@ -256,10 +333,7 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
             }
         };
 
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < blocks) load.issue(begin + 32 * i, i);
-        mfma::wait_async_loads();
+        load.start();
         barrier();
         read_keys(0);
         read_values(0);
@@ -271,12 +345,7 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
             weigh(0, 0, 8);
         }
         const auto step = [&](int i, auto last) {
-            if constexpr (!last.value) {
-                if (i + 2 < blocks) mfma::wait_async_loads_keep<Loader<kD, kCodes>::kInFlight>();
-                else mfma::wait_async_loads();
-                barrier();
-                if (i + 3 < blocks) load.issue(begin + 32 * (i + 3), (i + 3) % kRing);
-            }
+            if constexpr (!last.value) load.turn(i);
             if constexpr (kSets == 2) {
                 half_step(std::integral_constant<int, 0>(), i, i + 1, last);
                 half_step(std::integral_constant<int, 1>(), i + 1, i + 1, last);
@@ -285,6 +354,8 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
                 refer(0, largest(0));
                 weigh(0, 0, 8);
                 if constexpr (!last.value) {
+                    load.slice(0, i);
+                    load.slice(1, i);
                     read_keys(i + 1);
                     logits(0);
                 }
@@ -328,15 +399,11 @@ hipError_t launch_attend_chunk(const AttendArgs &a, const AttendPlan &p, float2 
     const int heads = a.B * a.Hkv, classes = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
     const long long per_head = (long long)p.tiles * p.splits, line = (per_head + 8 / classes - 1) / (8 / classes);
     const dim3 grid((unsigned)(8 * line * (heads / classes)));
-    const auto go = [&](auto dim, auto sets) {
-        attend_chunk<dim.value, sets.value, false><<<grid, kThreads, 0, stream>>>(a, p, part_ml, part_o);
+    return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto, auto codes) {
+        if (p.tile_rows == 256) attend_chunk<dim.value, 2, codes.value><<<grid, kThreads, 0, stream>>>(a, p, part_ml, part_o);
+        else attend_chunk<dim.value, 1, codes.value><<<grid, kThreads, 0, stream>>>(a, p, part_ml, part_o);
         return hipGetLastError();
-    };
-    using std::integral_constant;
-    const auto by_sets = [&](auto dim) {
-        return p.tile_rows == 256 ? go(dim, integral_constant<int, 2>()) : go(dim, integral_constant<int, 1>());
-    };
-    return a.d == 128 ? by_sets(integral_constant<int, 128>()) : by_sets(integral_constant<int, 64>());
+    });
 }
 
 }  // namespace obc
