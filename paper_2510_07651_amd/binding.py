@@ -545,7 +545,6 @@ class KvCache:
         self._index = k.get_device()
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self._arg = _CacheArg(ptr(k), ptr(v), ptr(k_scale), ptr(v_scale), ptr(page_table), self.batch, P, pages, S, Hkv, d, codes[k.dtype])
-        self._ref = ctypes.pointer(self._arg)
 
     @classmethod
     def empty(cls, num_pages: int, Hkv: int, page_size: int, d: int, dtype=torch.bfloat16, page_table=None, device="cuda"):
@@ -558,31 +557,21 @@ class KvCache:
 
     def _ints(self, t: torch.Tensor, what: str, per_head: bool = True) -> int:
         """1 for lengths [B,Hkv], 0 for [B]."""
-        if t.dtype is _I32 and t.get_device() == self._index and t.is_contiguous() and t.is_cuda:
-            if t.shape == (self.batch,):
+        if t.dtype is _I32 and t.get_device() == self._index and t.is_contiguous():
+            shape = t.shape
+            if shape == (self.batch,):
                 return 0
-            if per_head and t.shape == (self.batch, self.Hkv):
+            if per_head and shape == (self.batch, self.Hkv):
                 return 1
         raise ValueError("%s must be contiguous int32 [B]%s on the cache's GPU" % (what, " or [B,Hkv]" if per_head else ""))
 
-    def _launch(self, call, *args):
+    def _launch(self, call, args):
         """call(*args, stream) on the current stream of the cache's GPU, with that one current."""
         index = self._index
         if index == torch.cuda.current_device():
             return call(*args, _raw_stream(index) if _raw_stream is not None else _stream_ptr(self.k))
         with torch.cuda.device(index):
             return call(*args, _stream_ptr(self.k))
-
-
-def _rows(t: torch.Tensor, heads: Optional[int], like: torch.Tensor, what: str) -> _RowsArg:
-    B, T, _, d = like.shape
-    if (t.dim() != 4 or t.shape[0] != B or t.shape[1] != T or t.shape[3] != d or heads is not None and t.shape[2] != heads
-            or t.dtype is not like.dtype or t.get_device() != like.get_device() or not t.is_cuda):
-        raise ValueError("%s must be [B,T,H,d] and fit the other rows and the cache" % what)
-    sb, st, sh, sd = t.stride()
-    if sd != 1 and d != 1:
-        raise ValueError("%s: the channels of a row must be contiguous" % what)
-    return _RowsArg(t.data_ptr(), sb, st, sh)
 
 
 def obc_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, q: Optional[torch.Tensor] = None,
@@ -593,42 +582,60 @@ def obc_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, lens: tor
     """k, v [B,T,Hkv,d] (and q [B,T,Hq,d]), any strides over whole rows, normed, rotated and written: k, v to rows lens - n .. lens - 1
     of the cache, q to q_out [B,Hq,T,d], which is returned.  lens [B] or [B,Hkv] int32 counts the new rows in; new_lens [B] int32
     (without q also [B,Hkv]): the first n of the T are new; positions [B,T] int32 and inv_freq [pairs] float32 turn on the rotation."""
-    if k.dim() != 4 or k.shape[0] != cache.batch or k.shape[2] != cache.Hkv or k.shape[3] != cache.d or k.get_device() != cache._index:
+    # (A call per layer and token, like obc_decode_step: nothing is asked twice.)
+    index, dtype, shape = cache._index, k.dtype, k.shape
+    if len(shape) != 4 or shape[0] != cache.batch or shape[2] != cache.Hkv or shape[3] != cache.d or k.get_device() != index:
         raise ValueError("k must be [B,T,Hkv,d] on the cache's GPU")
-    if k.dtype is not cache.dtype and cache.dtype is not _E4M3:
+    if dtype is not cache.dtype and cache.dtype is not _E4M3:
         raise ValueError("rows and cache must be of one type, or the cache of 8 bits")
-    B, T, _, d = k.shape
-    k_arg, v_arg = _rows(k, cache.Hkv, k, "k"), _rows(v, cache.Hkv, k, "v")
+    if v.shape != shape or v.dtype is not dtype or v.get_device() != index:
+        raise ValueError("v must be like k")
+    B, T, _, d = shape
+    kb, kt, kh, kc = k.stride()
+    vb, vt, vh, vc = v.stride()
+    if kc != 1 or vc != 1:
+        raise ValueError("the channels of a row must be contiguous")
     per_head = cache._ints(lens, "lens")
     new_ptr, new_per_head = (None, 0) if new_lens is None else (new_lens.data_ptr(), cache._ints(new_lens, "new_lens", q is None))
-    q_arg, Hq = None, 0
+    q_arg, q_ptr, Hq = None, None, 0
     if q is not None:
-        q_arg = ctypes.byref(_rows(q, None, k, "q"))
-        Hq = q.shape[2]
+        q_shape = q.shape
+        if len(q_shape) != 4 or q_shape[0] != B or q_shape[1] != T or q_shape[3] != d or q.dtype is not dtype or q.get_device() != index:
+            raise ValueError("q must be [B,T,Hq,d] and fit k")
+        Hq = q_shape[2]
         if Hq < 1 or Hq % cache.Hkv:
             raise ValueError("q needs a multiple of Hkv heads")
+        qb, qt, qh, qc = q.stride()
+        if qc != 1:
+            raise ValueError("the channels of a row must be contiguous")
+        q_arg = _RowsArg(q.data_ptr(), qb, qt, qh)
         if q_out is None:
-            q_out = torch.empty((B, Hq, T, d), dtype=k.dtype, device=k.device)
-        elif q_out.shape != (B, Hq, T, d) or q_out.dtype is not k.dtype or q_out.get_device() != cache._index or not q_out.is_contiguous():
+            q_out = torch.empty((B, Hq, T, d), dtype=dtype, device=k.device)
+        elif q_out.shape != (B, Hq, T, d) or q_out.dtype is not dtype or q_out.get_device() != index or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous [B,Hq,T,d] of q's type")
+        q_ptr = q_out.data_ptr()
     elif q_out is not None or q_norm is not None:
         raise ValueError("q_out and q_norm belong to q")
-    if (positions is None) != (inv_freq is None):
-        raise ValueError("positions and inv_freq belong together")
-    pairs = 0
-    if inv_freq is not None:
+    pos_ptr, freq_ptr, pairs = None, None, 0
+    if inv_freq is not None and positions is not None:
         pairs = inv_freq.numel()
-        if (inv_freq.dtype is not _F32 or inv_freq.get_device() != cache._index or not inv_freq.is_contiguous() or positions.dtype is not _I32
-                or positions.shape != (B, T) or positions.get_device() != cache._index or not positions.is_contiguous() or pairs < 1):
+        if (inv_freq.dtype is not _F32 or inv_freq.get_device() != index or not inv_freq.is_contiguous() or positions.dtype is not _I32
+                or positions.shape != (B, T) or positions.get_device() != index or not positions.is_contiguous() or pairs < 1):
             raise ValueError("positions must be contiguous [B,T] int32, inv_freq [pairs] float32, on the cache's GPU")
-    for w in (q_norm, k_norm):
-        if w is not None and (w.shape != (d,) or w.dtype is not k.dtype or w.get_device() != cache._index or not w.is_contiguous()):
-            raise ValueError("q_norm, k_norm must be contiguous [d] of the rows' type")
-    rc = cache._launch((_lib or load_library()).obc_cache_append, q_arg, ctypes.byref(k_arg), ctypes.byref(v_arg), cache._ref,
-                       None if q_out is None else q_out.data_ptr(), lens.data_ptr(), per_head, new_ptr, new_per_head,
-                       None if positions is None else positions.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(), pairs,
-                       rot_scale, 1 if interleaved else 0, None if q_norm is None else q_norm.data_ptr(),
-                       None if k_norm is None else k_norm.data_ptr(), eps, B, T, Hq, OBC_BF16 if k.dtype is _BF16 else _dtype_code(k))
+        pos_ptr, freq_ptr = positions.data_ptr(), inv_freq.data_ptr()
+    elif inv_freq is not None or positions is not None:
+        raise ValueError("positions and inv_freq belong together")
+    norms = [None, None]
+    if q_norm is not None or k_norm is not None:
+        for i, w in enumerate((q_norm, k_norm)):
+            if w is not None:
+                if w.shape != (d,) or w.dtype is not dtype or w.get_device() != index or not w.is_contiguous():
+                    raise ValueError("q_norm, k_norm must be contiguous [d] of the rows' type")
+                norms[i] = w.data_ptr()
+    rc = cache._launch((_lib or load_library()).obc_cache_append, (
+        q_arg, _RowsArg(k.data_ptr(), kb, kt, kh), _RowsArg(v.data_ptr(), vb, vt, vh), cache._arg, q_ptr, lens.data_ptr(), per_head, new_ptr,
+        new_per_head, pos_ptr, freq_ptr, pairs, rot_scale, 1 if interleaved else 0, norms[0], norms[1], eps, B, T, Hq,
+        OBC_BF16 if dtype is _BF16 else _dtype_code(k)))
     if rc != OBC_OK:
         raise ObcError(rc, "obc_cache_append")
     return q_out
@@ -640,7 +647,7 @@ def obc_attend_workspace_bytes(B: int, T: int, Hq: int, cache: KvCache, dtype) -
     code = {_F32: OBC_F32, _BF16: OBC_BF16}.get(dtype, dtype)
     if not isinstance(code, int):
         raise TypeError("queries are float32 or bfloat16, got %s" % dtype)
-    rc = load_library().obc_attend_workspace_bytes(B, T, Hq, cache._ref, code, ctypes.byref(out))
+    rc = load_library().obc_attend_workspace_bytes(B, T, Hq, cache._arg, code, ctypes.byref(out))
     if rc != OBC_OK:
         raise ObcError(rc, "obc_attend_workspace_bytes")
     return int(out.value)
@@ -670,9 +677,9 @@ def obc_attend(q: torch.Tensor, cache: KvCache, lens: torch.Tensor, new_lens: Op
         workspace = torch.empty(obc_attend_workspace_bytes(B, T, Hq, cache, code), dtype=_U8, device=q.device)
     elif not (workspace.is_cuda and workspace.is_contiguous() and workspace.get_device() == cache._index):
         raise ValueError("workspace must be contiguous and on the cache's GPU")
-    rc = cache._launch((_lib or load_library()).obc_attend, q.data_ptr(), cache._ref, out.data_ptr(), lens.data_ptr(), per_head,
-                       None if new_lens is None else new_lens.data_ptr(), B, T, Hq, code, 1 if causal else 0,
-                       d ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    rc = cache._launch((_lib or load_library()).obc_attend, (
+        q.data_ptr(), cache._arg, out.data_ptr(), lens.data_ptr(), per_head, None if new_lens is None else new_lens.data_ptr(), B, T, Hq, code,
+        1 if causal else 0, d ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel() * workspace.element_size()))
     if rc != OBC_OK:
         raise ObcError(rc, "obc_attend")
     return out
@@ -707,8 +714,9 @@ def obc_cache_read(cache: KvCache, n: Optional[int] = None, keep_idx: Optional[t
         elif x.shape != shape or x.dtype is not dtype or x.get_device() != cache._index or not x.is_contiguous():
             raise ValueError("k_out, v_out must be contiguous [B,Hkv,n,d] of one type on the cache's GPU")
         outs.append(x)
-    rc = cache._launch((_lib or load_library()).obc_cache_read, cache._ref, None if keep_idx is None else keep_idx.data_ptr(),
-                       outs[0].data_ptr(), outs[1].data_ptr(), cache.batch, n, OBC_F32 if dtype is _F32 else OBC_BF16)
+    rc = cache._launch((_lib or load_library()).obc_cache_read, (
+        cache._arg, None if keep_idx is None else keep_idx.data_ptr(), outs[0].data_ptr(), outs[1].data_ptr(), cache.batch, n,
+        OBC_F32 if dtype is _F32 else OBC_BF16))
     if rc != OBC_OK:
         raise ObcError(rc, "obc_cache_read")
     return outs[0], outs[1]

@@ -129,40 +129,38 @@ __global__ __launch_bounds__(256) void attend_plain(AttendArgs a, AttendPlan pla
                 make_float4(o[cb][4 * j], o[cb][4 * j + 1], o[cb][4 * j + 2], o[cb][4 * j + 3]);
 }
 
-// Joins the shares of a row: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  One workgroup per row; 256 / (d / 4) shares at a time.
-template <int kD, int kDtype>
+// Joins the shares of a row: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  d / 4 lanes hold a row; a workgroup takes 256 / (d / 4) shares of one
+// row at a time or, where rows have few shares, as many rows.
+template <int kD, int kDtype, bool kManyRows>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a, AttendPlan plan, const float2 *part_ml, const float *part_o) {
     constexpr int kLanes = kD / 4, kSlots = 256 / kLanes, kSize = kDtype == OBC_BF16 ? 2 : 4;
-    __shared__ float4 sums[kSlots][kLanes];
-    __shared__ float2 ml[kSlots];
-    const int rows = a.G * a.T;
-    const int bg = blockIdx.x / rows, row = blockIdx.x % rows;
+    const int rows = a.G * a.T, slot = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+    const int at = kManyRows ? blockIdx.x * kSlots + slot : blockIdx.x;
+    if (kManyRows && at >= a.B * a.Hkv * rows) return;
+    const int bg = at / rows, row = at % rows;
     const Tile x = tile_of(a, bg, row / plan.tile_rows * plan.tile_rows, plan.tile_rows);
     const int share = share_of(x.seen, plan.splits, plan.min_share);
     const int shares = max((x.seen + share - 1) / share, 1);
-    const int slot = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
     float top = kNone, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = slot; s < shares; s += kSlots) {
+    const auto add = [&](const float2 m, const float4 o) {
+        const float now = fmaxf(top, m.x), old = __builtin_amdgcn_exp2f(top - now), w = __builtin_amdgcn_exp2f(m.x - now);
+        top = now;
+        sum = sum * old + m.y * w;
+        acc.x = acc.x * old + o.x * w; acc.y = acc.y * old + o.y * w; acc.z = acc.z * old + o.z * w; acc.w = acc.w * old + o.w * w;
+    };
+    for (int s = kManyRows ? 0 : slot; s < shares; s += kManyRows ? 1 : kSlots) {
         const size_t rec = ((size_t)s * a.B * a.Hkv + bg) * rows + row;
-        const float2 m = part_ml[rec];
-        const float4 o = *(const float4 *)(part_o + rec * kD + 4 * c);
-        const float now = fmaxf(top, m.x), old = __builtin_amdgcn_exp2f(top - now), w = __builtin_amdgcn_exp2f(m.x - now);
-        top = now;
-        sum = sum * old + m.y * w;
-        acc.x = acc.x * old + o.x * w; acc.y = acc.y * old + o.y * w; acc.z = acc.z * old + o.z * w; acc.w = acc.w * old + o.w * w;
+        add(part_ml[rec], *(const float4 *)(part_o + rec * kD + 4 * c));
     }
-    sums[slot][c] = acc;
-    if (c == 0) ml[slot] = make_float2(top, sum);
-    __syncthreads();
-    if (slot != 0) return;
-    for (int s = 1; s < kSlots; ++s) {
-        const float2 m = ml[s];
-        const float4 o = sums[s][c];
-        const float now = fmaxf(top, m.x), old = __builtin_amdgcn_exp2f(top - now), w = __builtin_amdgcn_exp2f(m.x - now);
-        top = now;
-        sum = sum * old + m.y * w;
-        acc.x = acc.x * old + o.x * w; acc.y = acc.y * old + o.y * w; acc.z = acc.z * old + o.z * w; acc.w = acc.w * old + o.w * w;
+    if constexpr (!kManyRows) {
+        __shared__ float4 sums[kSlots][kLanes];
+        __shared__ float2 ml[kSlots];
+        sums[slot][c] = acc;
+        if (c == 0) ml[slot] = make_float2(top, sum);
+        __syncthreads();
+        if (slot != 0) return;
+        for (int s = 1; s < min(kSlots, shares); ++s) add(ml[s], sums[s][c]);
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     const int t = row / a.G, h = x.g * a.G + row % a.G;
@@ -182,14 +180,20 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
         p->form = kAttendToken;
         p->tile_rows = rows <= 16 ? 16 : 32;
         p->min_share = 128;
-        want = 1024;
+        // (us, 512 and 1024 workgroups: 64 x 8 heads x 1000 rows 42.5 and 49.6, 8 heads x 131072 101 and 105, 32 x 8 heads x 8192 ragged rows of
+        // 8 bits 70.9 and 72.5; shares of 128 and 256 tokens, 8 heads x 1025 8.4 and 9.8)
+        want = 512;
         least = 128;
     } else if (dtype == OBC_BF16) {
+        // Two workgroups per compute unit.  A share costs its sums' way through memory, and one of few blocks its start (us, 32/8 heads: 512 rows over
+        // 8192 in one share 101, in two 81; 1024 rows of 1024 in one 26.8, in two 33.3; 512 of 512 in one 16.4, in two 24.9; 16 over 8192
+        // in shares of 1024 34.0, of 512 21.5, of 256 18.5; 256 over 2048 in shares of 512 28.7, of 256 30.4).
+        const long long units = heads * ((rows + kAttendChunkRows - 1) / kAttendChunkRows);
         p->form = kAttendChunk;
-        p->tile_rows = heads * ((rows + 255) / 256) >= 128 ? 256 : 128;
+        p->tile_rows = kAttendChunkRows;
         p->min_share = 32;
-        want = p->tile_rows == 256 ? 256 : 512;
-        least = 256;
+        want = 512;
+        least = units >= 256 ? 2048 : units >= 64 ? 512 : 256;
     } else {
         p->form = kAttendPlain;
         p->tile_rows = 32;
@@ -224,7 +228,9 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, char *workspa
     }
     if (e != hipSuccess || p.splits == 1) return e;
     return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto) {
-        attend_join<dim.value, type.value><<<dim3((unsigned)(a.B * a.Hkv * a.G * a.T)), 256, 0, stream>>>(a, p, ml, o);
+        const int rows = a.B * a.Hkv * a.G * a.T, per = 1024 / dim.value;
+        if (p.splits <= 8) attend_join<dim.value, type.value, true><<<dim3((rows + per - 1) / per), 256, 0, stream>>>(a, p, ml, o);
+        else attend_join<dim.value, type.value, false><<<dim3(rows), 256, 0, stream>>>(a, p, ml, o);
         return hipGetLastError();
     });
 }

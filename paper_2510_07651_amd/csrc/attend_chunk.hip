@@ -10,7 +10,7 @@ using mfma::bf16x8;
 using mfma::f32x16;
 using mfma::i16x4;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kTileRows = kAttendChunkRows;
 constexpr int kRing = 4;               // blocks of 32 tokens in LDS
 constexpr float kLazy = 8.f;           // log2 of how far a weight may grow past its reference before sums are rescaled
 
@@ -160,57 +160,50 @@ struct Loader<kD, true> {
     }
 };
 
-// Workgroup of four waves, 32 kSets rows each, against a share of the sequence in blocks of 32 tokens.
-template <int kD, int kSets, bool kCodes>
-__global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
+// Workgroup of four waves, 32 rows each, against a share of the sequence in blocks of 32 tokens.  S^T = K Q^T and O^T = V^T P^T: a lane
+// holds one row's column of both, so the softmax needs one exchange between the wave's halves and no shuffle of P: register 4 j + i of
+// S^T is token 8 j + 4 half + i, and V's operand takes its tokens in that order.
+template <int kD, bool kCodes>
+__global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
     using S = Shape<kD>;
     __shared__ __attribute__((aligned(1024))) char smem[kRing * S::kSlot];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
 
     // Which tile: workgroups go to the eight dies in turn; those of one KV head stay on as few as there are heads for, so that they
-    // find its rows in that die's L2.  Late tiles, which see most, first.
+    // find its rows in that die's L2.  Late tiles, which see most, first (2048 rows of a prompt of 2048, 32/8 heads: 56.1 us, with those that share a
+    // compute unit folded 50.9; 1500 over 4000 106.0, 103.7).
     const int heads = a.B * a.Hkv, die = blockIdx.x & 7, classes = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
-    const int per_head = plan.tiles * plan.splits, line = (per_head + 8 / classes - 1) / (8 / classes);
-    const int at = (int)(blockIdx.x >> 3), place = die / classes + 8 / classes * (at % line);
-    const int bg = die % classes + classes * (at / line);
+    const int per_head = plan.tiles * plan.splits, line = (per_head + 8 / classes - 1) / (8 / classes), mine = heads / classes;
+    const int at = (int)(blockIdx.x >> 3);
+    int head = at / line, in_line = at % line;
+    if (mine * line <= 64) {                   // all at once, two per compute unit: the longest with the shortest
+        const int j = at < 32 ? at : mine * line - 1 - (at - 32);
+        head = j % mine;
+        in_line = j / mine;
+    }
+    const int place = die / classes + 8 / classes * in_line, bg = die % classes + classes * head;
     if (place >= per_head) return;
     const int tile = plan.tiles - 1 - place / plan.splits, split = place % plan.splits;
 
-    const Tile x = tile_of(a, bg, tile * plan.tile_rows, plan.tile_rows);
+    const Tile x = tile_of(a, bg, tile * kTileRows, kTileRows);
     const int share = share_of(x.seen, plan.splits, plan.min_share);
     const int begin = split * share, end = min(begin + share, x.seen), blocks = (end - begin + 31) / 32;
     if (blocks <= 0 && split > 0) return;
 
-    int row[kSets], seen[kSets], full[kSets];      // full: tokens that every row of the set that counts sees
-    bf16x8 q[kSets][S::kSteps];
+    const int r0 = x.r0 + wave * 32, row = r0 + col, t = row / a.G, h = x.g * a.G + row % a.G;
+    const bool exists = t < a.T;
+    const int seen = exists ? min(tokens_seen(x.len, x.n, t, a.causal), end) : 0;
+    const int full = r0 / a.G < x.n ? min(tokens_seen(x.len, x.n, r0 / a.G, a.causal), end) : 0;    // tokens that every row that counts sees
+    bf16x8 q[S::kSteps];
+    const char *q_row = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * S::kRow + half * 16;
 #pragma unroll
-    for (int s = 0; s < kSets; ++s) {
-        const int r0 = x.r0 + (wave * kSets + s) * 32;
-        row[s] = r0 + col;
-        const int t = row[s] / a.G, h = x.g * a.G + row[s] % a.G;
-        const bool exists = t < a.T;
-        seen[s] = exists ? min(tokens_seen(x.len, x.n, t, a.causal), end) : 0;
-        full[s] = r0 / a.G < x.n ? min(tokens_seen(x.len, x.n, r0 / a.G, a.causal), end) : 0;
-        const char *p = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * S::kRow + half * 16;
+    for (int k = 0; k < S::kSteps; ++k) q[k] = *(const bf16x8 *)(q_row + 32 * k);
+    f32x16 o[S::kCols];
 #pragma unroll
-        for (int k = 0; k < S::kSteps; ++k) q[s][k] = *(const bf16x8 *)(p + 32 * k);
-    }
-    f32x16 o[kSets][S::kCols], z[kSets];
-    float top[kSets], sum[kSets];
-    union Weights { uint32_t u[8]; bf16x8 v[2]; } w[kSets];
+    for (int c = 0; c < S::kCols; ++c) o[c] = mfma::zero16();
+    float top = kNone, sum = 0.f;
 #pragma unroll
-    for (int s = 0; s < kSets; ++s) {
-        top[s] = kNone;
-        sum[s] = 0.f;
-#pragma unroll
-        for (int c = 0; c < S::kCols; ++c) o[s][c] = mfma::zero16();
-#pragma unroll
-        for (int k = 0; k < S::kSteps; ++k) {
-            // (waits for the load here; queries of two sets are for the matrix cores alone and lie in the accumulator file)
-            if constexpr (kSets == 2) asm volatile("" : "+a"(q[s][k]));
-            else mfma::settle(q[s][k]);
-        }
-    }
+    for (int k = 0; k < S::kSteps; ++k) mfma::settle(q[k]);
 
     if (blocks > 0) {
         Loader<kD, kCodes> load(a.cache, x, begin, end, wave, lane, smem);
@@ -222,7 +215,7 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
             const int i = lane & 15, sub = (lane >> 4) & 1, R = 4 * half + (i >> 2);
             v_off[c] = S::kBlock + R * S::kRow + value_slot<kD>(R, c * 4 + sub * 2 + ((i & 3) >> 1)) * 16 + (i & 1) * 8;
         }
-        bf16x8 kb[S::kSteps], vb[S::kCols][2];
+        bf16x8 kb[S::kSteps], vb[2 * S::kCols];
         const auto read_keys = [&](int i) {
             const char *p = smem + (i % kRing) * S::kSlot;
 #pragma unroll
@@ -231,105 +224,50 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
         const auto read_values = [&](int i) {
             const char *p = smem + (i % kRing) * S::kSlot;
 #pragma unroll
-            for (int c = 0; c < S::kCols; ++c)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    union { bf16x8 v; i16x4 h[2]; } u;
-                    typedef __attribute__((address_space(3))) i16x4 *lds4;
-                    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + v_off[c] + 16 * k * S::kRow));
-                    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + v_off[c] + (16 * k + 8) * S::kRow));
-                    vb[c][k] = u.v;
-                }
+            for (int j = 0; j < 2 * S::kCols; ++j) {
+                union { bf16x8 v; i16x4 h[2]; } u;
+                typedef __attribute__((address_space(3))) i16x4 *lds4;
+                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + v_off[j / 2] + 16 * (j % 2) * S::kRow));
+                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + v_off[j / 2] + (16 * (j % 2) + 8) * S::kRow));
+                vb[j] = u.v;
+            }
         };
-        const auto logits = [&](int s) {
-            z[s] = mfma::zero16();
-#pragma unroll
-            for (int k = 0; k < S::kSteps; ++k) z[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[k], q[s][k], z[s], 0, 0, 0);
-        };
-        const auto output = [&](int s, int j) {
-            o[s][j / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j / 2][j % 2], w[s].v[j % 2], o[s][j / 2], 0, 0, 0);
-        };
-        // Hides what a row does not see.
-        const auto hide = [&](int s, int i) {
+        f32x16 z, z_next;
+        union { uint32_t u[8]; bf16x8 v[2]; } w;
+        const auto slot_end = [] { __builtin_amdgcn_sched_barrier(0); };
+        const auto logit = [&](f32x16 &to, int k) { to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[k], q[k], to, 0, 0, 0); };
+        const auto output = [&](int j) { o[j / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j], w.v[j % 2], o[j / 2], 0, 0, 0); };
+        // Hides what a row does not see of block i; the largest logit that is left, in log2.
+        const auto largest = [&](f32x16 &of, int i) {
             const int t0 = begin + 32 * i;
-            if (t0 + 32 > full[s]) {
+            if (t0 + 32 > full) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z[s][r] = t0 + 8 * (r / 4) + 4 * half + r % 4 < seen[s] ? z[s][r] : -__builtin_inff();
+                for (int r = 0; r < 16; ++r) of[r] = t0 + 8 * (r / 4) + 4 * half + r % 4 < seen ? of[r] : -__builtin_inff();
+            }
+            float most = mfma::max3(of[0], of[1], of[2]);
+#pragma unroll
+            for (int r = 3; r < 15; r += 2) most = mfma::max3(most, of[r], of[r + 1]);
+            return mfma::halves_max(fmaxf(most, of[15])) * a.scale_log2;
+        };
+        // Moves the row's reference if a logit has outgrown it.
+        const auto refer = [&](float most) {
+            if (__any(most > top + kLazy)) {
+                const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
+                top = now;
+                sum *= shrink;
+#pragma unroll
+                for (int c = 0; c < S::kCols; ++c) o[c] *= shrink;
             }
         };
-        const auto largest = [&](int s) {
-            float most = mfma::max3(z[s][0], z[s][1], z[s][2]);
-#pragma unroll
-            for (int r = 3; r < 15; r += 2) most = mfma::max3(most, z[s][r], z[s][r + 1]);
-            return mfma::halves_max(fmaxf(most, z[s][15])) * a.scale_log2;
-        };
-        // Moves a row's reference if a logit has outgrown it.  (The sums stay in the accumulator file: without the ties the compiler
-        // carries a copy of them around the loop for this branch, 64 moves per block.)
-        const auto refer = [&](int s, float most) {
-            if (__any(most > top[s] + kLazy)) {
-                const float now = fmaxf(top[s], most), shrink = __builtin_amdgcn_exp2f(top[s] - now);
-                top[s] = now;
-                sum[s] *= shrink;
-#pragma unroll
-                for (int c = 0; c < S::kCols; ++c) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[s][c][r] *= shrink;
-                    
-                }
-            }
-        };
-        // Weights of the set's pairs from .. to - 1 of eight: two tokens each.
+        // Weights of the pairs from .. to - 1 of eight: two tokens each.  Their sum is taken of what they are rounded to.
         const mfma::bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
-        const auto weigh = [&](int s, int from, int to) {
+        const auto weigh = [&](int from, int to) {
 #pragma unroll
             for (int j = from; j < to; ++j) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(z[s][2 * j], a.scale_log2, -top[s]));
-                const float f = __builtin_amdgcn_exp2f(fmaf(z[s][2 * j + 1], a.scale_log2, -top[s]));
-                w[s].u[j] = mfma::pack_bf16(e, f);
-                sum[s] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2, w[s].u[j]), one, sum[s], false);
-            }
-        };
-        // Half a step with two sets: the matrix cores add set `s`'s weights times this block's values and form its logits of the next
-        // block, while the vector ALUs turn the other set's logits into weights.  One matrix op and a slice of vector work per slot.
-        const auto half_step = [&](auto set, int block_other, int next, auto last) {
-            constexpr int s = set.value, u = 1 - s, kOut = 2 * S::kCols;
-            const auto slot_end = [] { __builtin_amdgcn_sched_barrier(0); };
-            output(s, 0);
-            if constexpr (s == 0 && !last.value) read_keys(next);
-            if constexpr (s == 0 && !last.value) load.slice(0, block_other);
-            slot_end();
-            output(s, 1);
-            if constexpr (s == 0 && !last.value) load.slice(1, block_other);
-            slot_end();
-            constexpr bool kNoOther = s == 1 && last.value;          // (the last block has nobody's next logits)
-            float most = 0.f;
-            if constexpr (!kNoOther) hide(u, block_other);
-            output(s, 2);
-            if constexpr (!kNoOther) most = largest(u);
-            output(s, 3);
-            if constexpr (!kNoOther) refer(u, most);
-            slot_end();
-            constexpr int kLeft = kOut - 4;
-            if constexpr (kLeft > 0) {
-#pragma unroll
-                for (int j = 0; j < kLeft; ++j) {
-                    output(s, 4 + j);
-                    if constexpr (!kNoOther) weigh(u, j / 2, (j + 1) / 2);
-                    slot_end();
-                }
-            }
-            if constexpr (!last.value) {
-                if constexpr (s == 1) read_values(next);
-                z[s] = mfma::zero16();
-#pragma unroll
-                for (int k = 0; k < S::kSteps; ++k) {
-                    z[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[k], q[s][k], z[s], 0, 0, 0);
-                    constexpr int kDone = kLeft / 2;
-                    weigh(u, kDone + k * (8 - kDone) / S::kSteps, kDone + (k + 1) * (8 - kDone) / S::kSteps);
-                    slot_end();
-                }
-            } else if constexpr (!kNoOther) {
-                weigh(u, kLeft / 2, 8);
+                const float e = __builtin_amdgcn_exp2f(fmaf(z[2 * j], a.scale_log2, -top));
+                const float f = __builtin_amdgcn_exp2f(fmaf(z[2 * j + 1], a.scale_log2, -top));
+                w.u[j] = mfma::pack_bf16(e, f);
+                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2, w.u[j]), one, sum, false);
             }
         };
 
@@ -337,60 +275,62 @@ __global__ __launch_bounds__(kThreads, kSets == 2 ? 1 : 2) void attend_chunk(Att
         barrier();
         read_keys(0);
         read_values(0);
+        z = mfma::zero16();
 #pragma unroll
-        for (int s = 0; s < kSets; ++s) logits(s);
-        if constexpr (kSets == 2) {
-            hide(0, 0);
-            refer(0, largest(0));
-            weigh(0, 0, 8);
-        }
-        const auto step = [&](int i, auto last) {
-            if constexpr (!last.value) load.turn(i);
-            if constexpr (kSets == 2) {
-                half_step(std::integral_constant<int, 0>(), i, i + 1, last);
-                half_step(std::integral_constant<int, 1>(), i + 1, i + 1, last);
-            } else {
-                hide(0, i);
-                refer(0, largest(0));
-                weigh(0, 0, 8);
-                if constexpr (!last.value) {
-                    load.slice(0, i);
-                    load.slice(1, i);
-                    read_keys(i + 1);
-                    logits(0);
-                }
+        for (int k = 0; k < S::kSteps; ++k) logit(z, k);
+        float most = largest(z, 0);
+        // Step i: the next block's logits beside this one's weights, one matrix op and a slice of vector work per slot, then this
+        // block's outputs beside the largest of those logits.
+        for (int i = 0; i + 1 < blocks; ++i) {
+            load.turn(i);
+            read_keys(i + 1);
+            load.slice(0, i);
+            load.slice(1, i);
+            refer(most);
+            slot_end();
+            // (8-bit rows leave the vector ALUs more to do outside the slots: a wave inside them goes first.  2 x 509 rows over 20011 tokens, 28/4 heads:
+            // 324 us without, 300 with; bf16 rows 497 us without, 516 with, 2048 rows over 16384.)
+            if constexpr (kCodes) __builtin_amdgcn_s_setprio(1);
+            z_next = mfma::zero16();
 #pragma unroll
-                for (int j = 0; j < 2 * S::kCols; ++j) output(0, j);
-                if constexpr (!last.value) read_values(i + 1);
+            for (int k = 0; k < S::kSteps; ++k) {
+                logit(z_next, k);
+                weigh(k * 8 / S::kSteps, (k + 1) * 8 / S::kSteps);
+                slot_end();
             }
-        };
-        for (int i = 0; i + 1 < blocks; ++i) step(i, std::false_type());
-        step(blocks - 1, std::true_type());
+#pragma unroll
+            for (int j = 0; j < S::kCols; ++j) output(j);
+            slot_end();
+            most = largest(z_next, i + 1);
+#pragma unroll
+            for (int j = S::kCols; j < 2 * S::kCols; ++j) output(j);
+            if constexpr (kCodes) __builtin_amdgcn_s_setprio(0);
+            z = z_next;
+            read_values(i + 1);
+        }
+        refer(most);
+        weigh(0, 8);
+#pragma unroll
+        for (int j = 0; j < 2 * S::kCols; ++j) output(j);
     }
 
+    // (rows behind the chunk's end share a tile with rows that see something: what they have summed up is dropped here)
+    const bool sees = seen > 0, whole = plan.splits == 1;
+    const float both = mfma::halves_sum(sum), total = sees ? both : 0.f, by = !sees ? 0.f : whole ? 1.f / total : 1.f;
+    if (!exists) return;
+    const size_t rec = ((size_t)split * heads + bg) * ((size_t)a.G * a.T) + row;
+    if (!whole && half == 0) part_ml[rec] = make_float2(sees ? top : kNone, total);
 #pragma unroll
-    for (int s = 0; s < kSets; ++s) {
-        // (rows behind the chunk's end share a set with rows that see something: what they have summed up is dropped here)
-        const bool sees = seen[s] > 0;
-        const float both = mfma::halves_sum(sum[s]), total = sees ? both : 0.f;
-        const int t = row[s] / a.G, h = x.g * a.G + row[s] % a.G;
-        if (t >= a.T) continue;
-        const bool whole = plan.splits == 1;
-        const float by = !sees ? 0.f : whole ? 1.f / total : 1.f;
-        const size_t rec = ((size_t)split * heads + bg) * ((size_t)a.G * a.T) + row[s];
-        if (!whole && half == 0) part_ml[rec] = make_float2(sees ? top[s] : kNone, total);
+    for (int c = 0; c < S::kCols; ++c)
 #pragma unroll
-        for (int c = 0; c < S::kCols; ++c)
+        for (int j = 0; j < 4; ++j) {
+            const int ch = 32 * c + 8 * j + 4 * half;
+            float y[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int ch = 32 * c + 8 * j + 4 * half;
-                float y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = sees ? o[s][c][4 * j + i] * by : 0.f;
-                if (whole) store4<OBC_BF16>(a.out + ((((size_t)x.b * a.T + t) * a.Hq + h) * kD + ch) * 2, y);
-                else store4<OBC_F32>((char *)(part_o + rec * kD + ch), y);
-            }
-    }
+            for (int i = 0; i < 4; ++i) y[i] = sees ? o[c][4 * j + i] * by : 0.f;
+            if (whole) store4<OBC_BF16>(a.out + ((((size_t)x.b * a.T + t) * a.Hq + h) * kD + ch) * 2, y);
+            else store4<OBC_F32>((char *)(part_o + rec * kD + ch), y);
+        }
 }
 
 }  // namespace
@@ -400,8 +340,7 @@ hipError_t launch_attend_chunk(const AttendArgs &a, const AttendPlan &p, float2 
     const long long per_head = (long long)p.tiles * p.splits, line = (per_head + 8 / classes - 1) / (8 / classes);
     const dim3 grid((unsigned)(8 * line * (heads / classes)));
     return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto, auto codes) {
-        if (p.tile_rows == 256) attend_chunk<dim.value, 2, codes.value><<<grid, kThreads, 0, stream>>>(a, p, part_ml, part_o);
-        else attend_chunk<dim.value, 1, codes.value><<<grid, kThreads, 0, stream>>>(a, p, part_ml, part_o);
+        attend_chunk<dim.value, codes.value><<<grid, kThreads, 0, stream>>>(a, p, part_ml, part_o);
         return hipGetLastError();
     });
 }
