@@ -11,6 +11,7 @@
 namespace obc {
 
 constexpr int kAttendChunkRows = 128;  // rows per workgroup of attend_chunk
+constexpr float kLazy = 8.f;           // log2 of how far a weight may grow past its reference before sums are rescaled
 constexpr float kNone = -3.0e38f;      // running maximum of a row that has seen nothing: finite, so that differences stay numbers
 
 // Tokens the rows of new token t see of a KV head with `len` rows, `n` of them new.

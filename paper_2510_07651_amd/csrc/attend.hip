@@ -8,14 +8,19 @@ namespace {
 
 using mfma::f32x16;
 
-// The general kernel, in fp32: one wave per (tile of 32 rows, share).  S^T = K Q^T and O^T = V^T P^T on the fp32 matrix cores: a
+// fp32 queries, everything in fp32: one wave per (tile of 32 rows, share).  S^T = K Q^T and O^T = V^T P^T on the fp32 matrix cores: a
 // lane holds one row's column of both, so the softmax needs one exchange between the wave's halves and no shuffle of P:
-// register 4 j + i of S^T is token 8 j + 4 half + i, and as long as V's operand takes its tokens in that order the product is the same.
-template <int kD, int kDtype, bool kCodes>
-__global__ __launch_bounds__(256) void attend_plain(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
+// register 4 j + i of S^T is token 8 j + 4 half + i, and V's operand takes its tokens in that order, its lane l channels
+// (d / 32) l .. of a row, which 32 lanes read whole.
+//
+// Bound by the matrix cores from 32 rows per KV head on (8192 cycles per 32 tokens, d = 128; one wave per SIMD, since queries, sums, and
+// the keys and values of the next block take 256 registers), by the cache's way from memory below.
+template <int kD, bool kCodes>
+__global__ __launch_bounds__(256, 1) void attend_fp32(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
+    constexpr int kE = kD / 32, kScales = kD / kScaleBlock, kRow = kCodes ? kD : 4 * kD;
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int units = plan.tiles * plan.splits * a.B * a.Hkv;
-    const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= units) return;
     const int split = unit % plan.splits, tile = unit / plan.splits % plan.tiles, bg = unit / (plan.splits * plan.tiles);
     const Tile x = tile_of(a, bg, tile * 32, 32);
@@ -23,110 +28,123 @@ __global__ __launch_bounds__(256) void attend_plain(AttendArgs a, AttendPlan pla
     const int begin = split * share, end = min(begin + share, x.seen);
     if (begin >= end && split > 0) return;
 
-    constexpr int kSize = kDtype == OBC_BF16 ? 2 : 4;
     const int row = x.r0 + col, t = row / a.G, h = x.g * a.G + row % a.G;
     const bool exists = t < a.T;
-    const int seen = exists ? tokens_seen(x.len, x.n, t, a.causal) : 0;
-    float q[kD / 2];             // channels 8 s + 4 half + i
-    const char *q_row = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * (kD * kSize);
+    const int seen = exists ? min(tokens_seen(x.len, x.n, t, a.causal), end) : 0;
+    const int full = x.r0 / a.G < x.n ? min(tokens_seen(x.len, x.n, x.r0 / a.G, a.causal), end) : 0;
+    float4 q[kD / 8];             // channels 8 s + 4 half ..
+    const char *q_row = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * (kD * 4) + 16 * half;
 #pragma unroll
-    for (int s = 0; s < kD / 8; ++s) {
-        const char *p = q_row + (8 * s + 4 * half) * kSize;
-        if constexpr (kDtype == OBC_BF16) {
-            const u32x2 w = *(const u32x2 *)p;
-            q[4 * s] = __uint_as_float(w[0] << 16); q[4 * s + 1] = __uint_as_float(w[0] & 0xffff0000u);
-            q[4 * s + 2] = __uint_as_float(w[1] << 16); q[4 * s + 3] = __uint_as_float(w[1] & 0xffff0000u);
-        } else {
-            *(float4 *)(q + 4 * s) = *(const float4 *)p;
-        }
-    }
-    f32x16 o[kD / 32];
+    for (int s = 0; s < kD / 8; ++s) q[s] = *(const float4 *)(q_row + 32 * s);
+    f32x16 o[kE];
 #pragma unroll
-    for (int cb = 0; cb < kD / 32; ++cb) o[cb] = mfma::zero16();
+    for (int e = 0; e < kE; ++e) o[e] = mfma::zero16();
     float top = kNone, sum = 0.f;
 
+    // A block's rows as they lie in the cache, one block ahead; lane l (and l + 32) knows where row l % 32 of a block lies.  Rows past
+    // the end: the last one again, with weight 0.
+    const auto row_of = [&](int t0) -> unsigned long long {
+        const int j = min(t0 + col, end - 1);
+        return row_in_pool(a.cache, page_of(a.cache, x.b, j), x.g, j);
+    };
+    float4 k[kCodes ? 1 : kD / 8];
+    uint32_t k8[kCodes ? kD / 8 : 1], k_scale = 0;
+    float v[kCodes ? 1 : 16][kE];
+    uint32_t v8[kCodes ? 16 : 1], v_scale[kCodes ? 16 : 1];
+    const auto load_keys = [&](unsigned long long at) {
+        const char *p = a.cache.k + at * kRow + (kCodes ? 4 : 16) * half;
+#pragma unroll
+        for (int s = 0; s < kD / 8; ++s) {
+            if constexpr (kCodes) k8[s] = *(const uint32_t *)(p + 8 * s);
+            else k[s] = *(const float4 *)(p + 32 * s);
+        }
+        if constexpr (kCodes) k_scale = kScales == 4 ? *(const uint32_t *)(a.cache.k_scale + at * 4) : *(const uint16_t *)(a.cache.k_scale + at * 2);
+    };
+    const auto load_values = [&](unsigned long long at) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const unsigned long long of = __shfl(at, 8 * (r / 4) + 4 * half + r % 4);
+            const char *p = a.cache.v + of * kRow + kE * (kCodes ? 1 : 4) * col;
+            if constexpr (!kCodes && kE == 4) *(float4 *)v[r] = *(const float4 *)p;
+            else if constexpr (!kCodes) *(float2 *)v[r] = *(const float2 *)p;
+            else v8[r] = kE == 4 ? *(const uint32_t *)p : *(const uint16_t *)p;
+            if constexpr (kCodes) v_scale[r] = a.cache.v_scale[of * kScales + col * kE / kScaleBlock];
+        }
+    };
+
+    unsigned long long next = 0;
+    if (begin < end) {
+        const unsigned long long at = row_of(begin);
+        load_keys(at);
+        load_values(at);
+        next = row_of(begin + 32);
+    }
     for (int t0 = begin; t0 < end; t0 += 32) {
-        const int kt = min(t0 + col, end - 1);                       // (rows past the share's end: its last one again, weight 0)
-        const size_t krow = row_in_pool(a.cache, page_of(a.cache, x.b, kt), x.g, kt);
+        const bool more = t0 + 32 < end;
         f32x16 z = mfma::zero16();
 #pragma unroll
         for (int s = 0; s < kD / 8; ++s) {
-            float k[4];
-            const int lo = 8 * s + 4 * half;
-            if constexpr (kCodes) {
-                e4m3_values(*(const uint32_t *)(a.cache.k + krow * kD + lo), scale_value(a.cache.k_scale[krow * (kD / kScaleBlock) + s / 4]), k);
-            } else if constexpr (kDtype == OBC_BF16) {
-                const u32x2 w = *(const u32x2 *)(a.cache.k + krow * (kD * 2) + lo * 2);
-                k[0] = __uint_as_float(w[0] << 16); k[1] = __uint_as_float(w[0] & 0xffff0000u);
-                k[2] = __uint_as_float(w[1] << 16); k[3] = __uint_as_float(w[1] & 0xffff0000u);
-            } else {
-                *(float4 *)k = *(const float4 *)(a.cache.k + krow * (kD * 4) + lo * 4);
-            }
+            float y[4];
+            if constexpr (kCodes) e4m3_values(k8[s], scale_value((k_scale >> (8 * (s / 4))) & 0xffu), y);
+            else *(float4 *)y = k[s];
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(y[0], q[s].x, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(y[1], q[s].y, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(y[2], q[s].z, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(y[3], q[s].w, z, 0, 0, 0);
+        }
+        if (more) load_keys(next);
+        if (t0 + 32 > full) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i], q[4 * s + i], z, 0, 0, 0);
+            for (int r = 0; r < 16; ++r) z[r] = t0 + 8 * (r / 4) + 4 * half + r % 4 < seen ? z[r] : -__builtin_inff();
         }
         float most = kNone;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int tok = t0 + 8 * (r / 4) + 4 * half + r % 4;
-            z[r] = tok < min(seen, end) ? z[r] * a.scale_log2 : -__builtin_inff();
-            most = fmaxf(most, z[r]);
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, z[r]);
+        most = mfma::halves_max(most) * a.scale_log2;
+        if (__any(most > top + kLazy)) {
+            const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            sum *= shrink;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) o[e] *= shrink;
         }
-        const float now = fmaxf(top, mfma::halves_max(most));
-        const float shrink = __builtin_amdgcn_exp2f(top - now);
-        top = now;
-        sum *= shrink;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            z[r] = __builtin_amdgcn_exp2f(z[r] - now);
+            z[r] = __builtin_amdgcn_exp2f(fmaf(z[r], a.scale_log2, -top));
             sum += z[r];
         }
 #pragma unroll
-        for (int cb = 0; cb < kD / 32; ++cb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[cb][r] *= shrink;
-#pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int vt = min(t0 + 8 * (r / 4) + 4 * half + r % 4, end - 1);
-            const size_t vrow = row_in_pool(a.cache, page_of(a.cache, x.b, vt), x.g, vt);
+            float y[4];
+            if constexpr (kCodes) {
+                e4m3_values(v8[r], scale_value(v_scale[r]), y);
+            } else {
 #pragma unroll
-            for (int cb = 0; cb < kD / 32; ++cb) {
-                float v;
-                const int ch = 32 * cb + col;
-                if constexpr (kCodes) {
-                    const uint32_t code = *(const uint8_t *)(a.cache.v + vrow * kD + ch);
-                    v = __builtin_amdgcn_cvt_f32_fp8((int)code, 0) * scale_value(a.cache.v_scale[vrow * (kD / kScaleBlock) + cb]);
-                } else if constexpr (kDtype == OBC_BF16) {
-                    v = bf16_bits_to_float(*(const uint16_t *)(a.cache.v + (vrow * kD + ch) * 2));
-                } else {
-                    v = *(const float *)(a.cache.v + (vrow * kD + ch) * 4);
-                }
-                o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[r], o[cb], 0, 0, 0);
+                for (int e = 0; e < kE; ++e) y[e] = v[r][e];
             }
+#pragma unroll
+            for (int e = 0; e < kE; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[e], z[r], o[e], 0, 0, 0);
+        }
+        if (more) {
+            load_values(next);
+            next = row_of(t0 + 64);
         }
     }
-    sum = mfma::halves_sum(sum);
+    const bool sees = seen > 0, whole = plan.splits == 1;
+    const float both = mfma::halves_sum(sum), total = sees ? both : 0.f, by = !sees ? 0.f : whole ? 1.f / total : 1.f;
     if (!exists) return;
-    if (plan.splits == 1) {
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        char *to = a.out + (((size_t)x.b * a.T + t) * a.Hq + h) * (kD * kSize);
-#pragma unroll
-        for (int cb = 0; cb < kD / 32; ++cb)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float y[4] = {o[cb][4 * j] * inv, o[cb][4 * j + 1] * inv, o[cb][4 * j + 2] * inv, o[cb][4 * j + 3] * inv};
-                store4<kDtype>(to + (32 * cb + 8 * j + 4 * half) * kSize, y);
-            }
-        return;
-    }
     const size_t rec = ((size_t)split * a.B * a.Hkv + bg) * ((size_t)a.G * a.T) + row;
-    if (half == 0) part_ml[rec] = make_float2(top, sum);
+    if (!whole && half == 0) part_ml[rec] = make_float2(sees ? top : kNone, total);
+    float *to = whole ? (float *)a.out + (((size_t)x.b * a.T + t) * a.Hq + h) * kD : part_o + rec * kD;
 #pragma unroll
-    for (int cb = 0; cb < kD / 32; ++cb)
+    for (int r = 0; r < 16; ++r) {
+        float y[kE];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *(float4 *)(part_o + rec * kD + 32 * cb + 8 * j + 4 * half) =
-                make_float4(o[cb][4 * j], o[cb][4 * j + 1], o[cb][4 * j + 2], o[cb][4 * j + 3]);
+        for (int e = 0; e < kE; ++e) y[e] = sees ? o[e][r] * by : 0.f;
+        float *p = to + kE * (8 * (r / 4) + 4 * half + r % 4);
+        if constexpr (kE == 4) *(float4 *)p = make_float4(y[0], y[1], y[2], y[3]);
+        else *(float2 *)p = make_float2(y[0], y[1]);
+    }
 }
 
 // Joins the shares of a row: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  d / 4 lanes hold a row; a workgroup takes 256 / (d / 4) shares of one
@@ -195,11 +213,13 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
         want = 512;
         least = units >= 256 ? 2048 : units >= 64 ? 512 : 256;
     } else {
-        p->form = kAttendPlain;
+        // One wave per SIMD, however short its share (us, 1024 waves and 2048: 4 x 8 heads x 8192 rows, G = 4, 55.5 and 64.1; 256 rows over 4096 172
+        // and 185; shares of 32 and 128 tokens: 8 heads x 1000 rows 15.5 and 29.7).
+        p->form = kAttendFp32;
         p->tile_rows = 32;
         p->min_share = 32;
-        want = 2048;
-        least = 128;
+        want = 1024;
+        least = 32;
     }
     p->tiles = (int)((rows + p->tile_rows - 1) / p->tile_rows);
     p->splits = (int)std::max(1LL, std::min(want / (heads * p->tiles), (capacity + least - 1) / least));
@@ -220,9 +240,9 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, char *workspa
     } else if (p.form == kAttendToken) {
         e = launch_attend_token(a, p, ml, o, stream);
     } else {
-        e = with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
+        e = with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto, auto codes) {
             const long long units = (long long)p.tiles * p.splits * a.B * a.Hkv;
-            attend_plain<dim.value, type.value, codes.value><<<dim3((unsigned)((units + 3) / 4)), 256, 0, stream>>>(a, p, ml, o);
+            attend_fp32<dim.value, codes.value><<<dim3((unsigned)((units + 3) / 4)), 256, 0, stream>>>(a, p, ml, o);
             return hipGetLastError();
         });
     }

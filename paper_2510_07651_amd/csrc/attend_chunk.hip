@@ -12,7 +12,6 @@ using mfma::i16x4;
 
 constexpr int kThreads = 256, kTileRows = kAttendChunkRows;
 constexpr int kRing = 4;               // blocks of 32 tokens in LDS
-constexpr float kLazy = 8.f;           // log2 of how far a weight may grow past its reference before sums are rescaled
 
 template <int kD>
 struct Shape {

@@ -16,7 +16,6 @@ using mfma::bf16x8;
 using mfma::f32x4;
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr float kLazy = 8.f;           // log2 of how far a weight may grow past its reference before sums are rescaled
 
 typedef const __attribute__((address_space(4))) int32_t *table_ptr;    // read through scalar loads
 

@@ -111,7 +111,7 @@ struct AttendArgs {
     float scale_log2;        // scale * log2(e)
 };
 // How a call is cut up: rows (query head, new token) of a KV head in tiles, tokens in `splits` shares.  Offsets into the workspace.
-enum { kAttendPlain = 0, kAttendChunk = 1, kAttendToken = 2 };
+enum { kAttendFp32 = 0, kAttendChunk = 1, kAttendToken = 2 };
 struct AttendPlan {
     int form;                // kernel
     int tiles, tile_rows, splits, min_share;
