@@ -34,10 +34,11 @@ __device__ __forceinline__ Tile tile_of(const AttendArgs &a, int bg, int r0, int
     x.seen = first <= last ? tokens_seen(x.len, x.n, last, a.causal) : 0;
     return x;
 }
-// Tokens per share of a tile: the same in the kernels that leave partial sums and in the one that joins them.
-__device__ __forceinline__ int share_of(int seen, int splits, int min_share) {
-    const int even = (seen + splits - 1) / splits;
-    return max((even + min_share - 1) / min_share * min_share, min_share);
+// Tokens per share of a tile: the same in the kernels that leave partial sums and in the one that joins them.  A sequence that is short
+// for its cache has fewer shares than the plan.
+__device__ __forceinline__ int share_of(int seen, const AttendPlan &p) {
+    const int even = (seen + p.splits - 1) / p.splits;
+    return max((even + p.step - 1) / p.step * p.step, p.min_share);
 }
 
 template <int kDtype>

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256, 1) void attend_fp32(AttendArgs a, AttendPlan p
     if (unit >= units) return;
     const int split = unit % plan.splits, tile = unit / plan.splits % plan.tiles, bg = unit / (plan.splits * plan.tiles);
     const Tile x = tile_of(a, bg, tile * 32, 32);
-    const int share = share_of(x.seen, plan.splits, plan.min_share);
+    const int share = share_of(x.seen, plan);
     const int begin = split * share, end = min(begin + share, x.seen);
     if (begin >= end && split > 0) return;
 
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, AttendPlan plan
     if (kManyRows && at >= a.B * a.Hkv * rows) return;
     const int bg = at / rows, row = at % rows;
     const Tile x = tile_of(a, bg, row / plan.tile_rows * plan.tile_rows, plan.tile_rows);
-    const int share = share_of(x.seen, plan.splits, plan.min_share);
+    const int share = share_of(x.seen, plan);
     const int shares = max((x.seen + share - 1) / share, 1);
     float top = kNone, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -197,7 +197,7 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
     if (dtype == OBC_BF16 && rows <= 32) {
         p->form = kAttendToken;
         p->tile_rows = rows <= 16 ? 16 : 32;
-        p->min_share = 128;
+        p->step = p->min_share = 128;
         // (us, 512 and 1024 workgroups: 64 x 8 heads x 1000 rows 42.5 and 49.6, 8 heads x 131072 101 and 105, 32 x 8 heads x 8192 ragged rows of
         // 8 bits 70.9 and 72.5; shares of 128 and 256 tokens, 8 heads x 1025 8.4 and 9.8)
         want = 512;
@@ -209,15 +209,16 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
         const long long units = heads * ((rows + kAttendChunkRows - 1) / kAttendChunkRows);
         p->form = kAttendChunk;
         p->tile_rows = kAttendChunkRows;
-        p->min_share = 32;
         want = 512;
         least = units >= 256 ? 2048 : units >= 64 ? 512 : 256;
+        p->step = 32;
+        p->min_share = 256;
     } else {
         // One wave per SIMD, however short its share (us, 1024 waves and 2048: 4 x 8 heads x 8192 rows, G = 4, 55.5 and 64.1; 256 rows over 4096 172
         // and 185; shares of 32 and 128 tokens: 8 heads x 1000 rows 15.5 and 29.7).
         p->form = kAttendFp32;
         p->tile_rows = 32;
-        p->min_share = 32;
+        p->step = p->min_share = 32;
         want = 1024;
         least = 32;
     }

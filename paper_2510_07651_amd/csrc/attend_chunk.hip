@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, Attend
     const int tile = plan.tiles - 1 - place / plan.splits, split = place % plan.splits;
 
     const Tile x = tile_of(a, bg, tile * kTileRows, kTileRows);
-    const int share = share_of(x.seen, plan.splits, plan.min_share);
+    const int share = share_of(x.seen, plan);
     const int begin = split * share, end = min(begin + share, x.seen), blocks = (end - begin + 31) / 32;
     if (blocks <= 0 && split > 0) return;
 

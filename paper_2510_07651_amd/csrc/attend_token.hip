@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_token(AttendArgs a, Attend
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const int split = blockIdx.x % plan.splits, bg = blockIdx.x / plan.splits;
     const Tile x = tile_of(a, bg, 0, plan.tile_rows);
-    const int share = share_of(x.seen, plan.splits, plan.min_share);
+    const int share = share_of(x.seen, plan);
     const int begin = split * share, end = min(begin + share, x.seen);
     if (begin >= end && split > 0) return;
     const CacheView &c = a.cache;

@@ -114,7 +114,8 @@ struct AttendArgs {
 enum { kAttendFp32 = 0, kAttendChunk = 1, kAttendToken = 2 };
 struct AttendPlan {
     int form;                // kernel
-    int tiles, tile_rows, splits, min_share;
+    int tiles, tile_rows, splits;
+    int step, min_share;     // a share: a multiple of `step` tokens, at least `min_share`
     size_t part_ml, part_o, total;
 };
 

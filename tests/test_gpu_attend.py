@@ -114,6 +114,21 @@ def test_attend_several_shares(dtype, kind, T, N):
 
 
 @pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("T", [1, 20, 140])
+def test_attend_short_sequences_in_a_large_cache(dtype, kind, T):
+    """Calls are cut up for what the cache could hold; most of the shares have nothing to do."""
+    _run(dtype, kind, 2, 4, 1, T, 128, 64, 64, [T, 600], seed=T)
+
+
+@pytest.mark.parametrize("dtype,kind", TYPES)
+def test_attend_padding_beside_rows_that_see_much(dtype, kind):
+    """Padded rows share a tile with rows that see several blocks, in one share and in several; their queries are NaN."""
+    _run(dtype, kind, 2, 8, 2, 60, 128, 64, 16, [900, 333], new=[23, 59], seed=2)
+    _run(dtype, kind, 2, 8, 2, 60, 64, 32, 4, [128, 100], new=[41, 1], seed=3)
+    _run(dtype, kind, 2, 8, 2, 6, 128, 64, 16, [900, 333], new=[2, 5], seed=4)
+
+
+@pytest.mark.parametrize("dtype,kind", TYPES)
 def test_attend_scale_and_large_logits(dtype, kind):
     """A scale of the caller's; logits of hundreds, where one token takes everything."""
     _run(dtype, kind, 1, 4, 2, 3, 128, 16, 8, [100], scale=0.3)
