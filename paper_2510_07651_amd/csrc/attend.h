@@ -42,9 +42,13 @@ __device__ __forceinline__ int share_of(int seen, const AttendPlan &p) {
 }
 
 template <int kDtype>
-__device__ __forceinline__ void store4(char *p, const float (&x)[4]) {
-    if constexpr (kDtype == OBC_BF16) *(u32x2 *)p = u32x2{bf16_pair_of(x[0], x[1]), bf16_pair_of(x[2], x[3])};
-    else *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]);
+__device__ __forceinline__ void store4(void *p, const float (&x)[4]) {
+    if constexpr (kDtype == OBC_BF16) {
+        const uint32_t w[2] = {bf16_pair_of(x[0], x[1]), bf16_pair_of(x[2], x[3])};
+        store_bytes<8, false>(p, w);
+    } else {
+        store_bytes<16, false>(p, x);
+    }
 }
 
 // Calls `f` with a kernel's compile-time choices.

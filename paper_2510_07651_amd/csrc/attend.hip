@@ -65,8 +65,7 @@ __global__ __launch_bounds__(256, 1) void attend_fp32(AttendArgs a, AttendPlan p
         for (int r = 0; r < 16; ++r) {
             const unsigned long long of = __shfl(at, 8 * (r / 4) + 4 * half + r % 4);
             const char *p = a.cache.v + of * kRow + kE * (kCodes ? 1 : 4) * col;
-            if constexpr (!kCodes && kE == 4) *(float4 *)v[r] = *(const float4 *)p;
-            else if constexpr (!kCodes) *(float2 *)v[r] = *(const float2 *)p;
+            if constexpr (!kCodes) load_bytes<4 * kE>(v[r], p);
             else v8[r] = kE == 4 ? *(const uint32_t *)p : *(const uint16_t *)p;
             if constexpr (kCodes) v_scale[r] = a.cache.v_scale[of * kScales + col * kE / kScaleBlock];
         }
@@ -86,7 +85,7 @@ __global__ __launch_bounds__(256, 1) void attend_fp32(AttendArgs a, AttendPlan p
         for (int s = 0; s < kD / 8; ++s) {
             float y[4];
             if constexpr (kCodes) e4m3_values(k8[s], scale_value((k_scale >> (8 * (s / 4))) & 0xffu), y);
-            else *(float4 *)y = k[s];
+            else y[0] = k[s].x, y[1] = k[s].y, y[2] = k[s].z, y[3] = k[s].w;
             z = __builtin_amdgcn_mfma_f32_32x32x2f32(y[0], q[s].x, z, 0, 0, 0);
             z = __builtin_amdgcn_mfma_f32_32x32x2f32(y[1], q[s].y, z, 0, 0, 0);
             z = __builtin_amdgcn_mfma_f32_32x32x2f32(y[2], q[s].z, z, 0, 0, 0);

@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, Attend
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = sees ? o[c][4 * j + i] * by : 0.f;
             if (whole) store4<OBC_BF16>(a.out + ((((size_t)x.b * a.T + t) * a.Hq + h) * kD + ch) * 2, y);
-            else store4<OBC_F32>((char *)(part_o + rec * kD + ch), y);
+            else store4<OBC_F32>(part_o + rec * kD + ch, y);
         }
 }
 

@@ -33,13 +33,6 @@ struct Values {
     u32x4 scale[2];                                                     // the scale bytes of four tokens each
 };
 
-template <int kWords>
-__device__ __forceinline__ void load_words(uint32_t (&to)[kWords], const char *p) {
-    if constexpr (kWords == 4) *(u32x4 *)to = *(const u32x4 *)p;
-    else if constexpr (kWords == 2) *(u32x2 *)to = *(const u32x2 *)p;
-    else to[0] = *(const uint32_t *)p;
-}
-
 // Workgroup of four waves: rows of one tile (at most 16 kSets), a share of the sequence, 32 tokens per wave in turn.
 template <int kD, int kSets, bool kCodes>
 __global__ __launch_bounds__(kThreads, 2) void attend_token(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
@@ -128,7 +121,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_token(AttendArgs a, Attend
                 const size_t row = block_row(t0 + 16 * h);
                 const char *p = c.v + row * kRow;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) load_words<V::kWords>(vv.x[4 * h + i], p + (uint32_t)(4 * quad * kRow + col * 4 * V::kWords + i * kRow));
+                for (int i = 0; i < 4; ++i) load_bytes<4 * V::kWords>(vv.x[4 * h + i], p + (uint32_t)(4 * quad * kRow + col * 4 * V::kWords + i * kRow));
                 if constexpr (kCodes) {
                     if constexpr (kScales == 4) {
                         vv.scale[h] = *(const u32x4 *)(c.v_scale + row * 4 + (uint32_t)(16 * quad));
@@ -145,7 +138,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_token(AttendArgs a, Attend
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const size_t row = row_of(t0 + 16 * h + 4 * quad + i);
-                load_words<V::kWords>(vv.x[4 * h + i], c.v + row * kRow + col * 4 * V::kWords);
+                load_bytes<4 * V::kWords>(vv.x[4 * h + i], c.v + row * kRow + col * 4 * V::kWords);
                 if constexpr (kCodes) vv.scale[h][i] = kScales == 4 ? *(const uint32_t *)(c.v_scale + row * 4) : *(const uint16_t *)(c.v_scale + row * 2);
             }
     };

@@ -76,6 +76,48 @@ __device__ __forceinline__ uint32_t bf16_pair_of(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair){lo, hi}, bf16_pair));   // to nearest even
 }
 
+// kBytes (4, 8 or a multiple of 16) between memory, as aligned as they are many, and a local array of any type.
+template <int kBytes>
+__device__ __forceinline__ void load_bytes(void *to, const void *p) {
+    if constexpr (kBytes == 4) {
+        const uint32_t x = *(const uint32_t *)p;
+        __builtin_memcpy(to, &x, 4);
+    } else if constexpr (kBytes == 8) {
+        const u32x2 x = *(const u32x2 *)p;
+        __builtin_memcpy(to, &x, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kBytes / 16; ++i) {
+            const u32x4 x = *((const u32x4 *)p + i);
+            __builtin_memcpy((char *)to + 16 * i, &x, 16);
+        }
+    }
+}
+// `kPast`: past the caches.
+template <int kBytes, bool kPast>
+__device__ __forceinline__ void store_bytes(void *p, const void *from) {
+    const auto put = [](auto *to, const auto &x) {
+        if constexpr (kPast) __builtin_nontemporal_store(x, to);
+        else *to = x;
+    };
+    if constexpr (kBytes == 4) {
+        uint32_t x;
+        __builtin_memcpy(&x, from, 4);
+        put((uint32_t *)p, x);
+    } else if constexpr (kBytes == 8) {
+        u32x2 x;
+        __builtin_memcpy(&x, from, 8);
+        put((u32x2 *)p, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kBytes / 16; ++i) {
+            u32x4 x;
+            __builtin_memcpy(&x, (const char *)from + 16 * i, 16);
+            put((u32x4 *)p + i, x);
+        }
+    }
+}
+
 // ---- what the calls hand to the launchers ----------------------------------------------------------------------------------
 struct RowsView {            // rows of d contiguous elements at base + b * batch + t * token + h * head (bytes)
     const char *base;

@@ -10,51 +10,47 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kGroups = kThreads / 16;       // 16 lanes hold one row
 
-// d / 16 consecutive channels of a row, in fp32.
-template <int kN>
-__device__ __forceinline__ void load_row(const char *p, bool bf16, float (&x)[kN]) {
-    if (bf16) {
+// kN consecutive channels of a row, in fp32.
+template <int kN, bool kBf16>
+__device__ __forceinline__ void load_row(const char *p, float (&x)[kN]) {
+    if constexpr (kBf16) {
         uint32_t w[kN / 2];
-        if constexpr (kN == 8) *(u32x4 *)w = *(const u32x4 *)p;
-        else *(u32x2 *)w = *(const u32x2 *)p;
+        load_bytes<2 * kN>(w, p);
 #pragma unroll
         for (int i = 0; i < kN / 2; ++i) {
             x[2 * i] = __uint_as_float(w[i] << 16);
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     } else {
-#pragma unroll
-        for (int i = 0; i < kN; i += 4) *(float4 *)(x + i) = *(const float4 *)(p + 4 * i);
+        load_bytes<4 * kN>(x, p);
     }
 }
-template <int kN>
-__device__ __forceinline__ void store_row(char *p, bool bf16, const float (&x)[kN]) {
-    if (bf16) {
+template <int kN, bool kBf16, bool kPast>
+__device__ __forceinline__ void store_row(char *p, const float (&x)[kN]) {
+    if constexpr (kBf16) {
         uint32_t w[kN / 2];
 #pragma unroll
         for (int i = 0; i < kN / 2; ++i) w[i] = bf16_pair_of(x[2 * i], x[2 * i + 1]);
-        if constexpr (kN == 8) *(u32x4 *)p = *(u32x4 *)w;
-        else *(u32x2 *)p = *(u32x2 *)w;
+        store_bytes<2 * kN, kPast>(p, w);
     } else {
-#pragma unroll
-        for (int i = 0; i < kN; i += 4) *(float4 *)(p + 4 * i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        store_bytes<4 * kN, kPast>(p, x);
     }
 }
 
 // One workgroup per new token (and per 16 * gridDim.y of its heads): a row of d channels lies in 16 lanes, so the sum of its
-// squares is four lane exchanges, and a lane keeps its channels' cosines and sines for all heads of the token.
+// squares is four lane exchanges, and a lane keeps its channels' norm weights, cosines and sines for all heads of the token.
 // The angle pos * f is reduced to a part of one turn in 64 bits: in fp32 the product alone would be off by 2^-24 of the angle,
 // 0.06 rad at a million tokens.
-template <int kD, int kDtype, bool kCodes>
+template <int kD, int kDtype, bool kCodes, bool kPast>
 __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
     constexpr int kN = kD / 16;
     constexpr bool kBf16 = kDtype == OBC_BF16;
     constexpr int kSize = kBf16 ? 2 : 4;
     __shared__ float2 turn[kD / 2];
     const int b = blockIdx.x / a.T, t = blockIdx.x % a.T;
-    const int group = threadIdx.x / 16, c = threadIdx.x % 16;
+    const int group = threadIdx.x / 16, c = threadIdx.x % 16, lo = kN * c;
     const int Hkv = a.cache.Hkv, rows = a.Hq + 2 * Hkv;
-    const int step = kGroups * gridDim.y;
+    const int first = blockIdx.y * kGroups + group, step = kGroups * gridDim.y;
     if (a.pairs) {
         for (int i = threadIdx.x; i < a.pairs; i += kThreads) {
             double turns = (double)a.positions[(size_t)b * a.T + t] * (double)a.inv_freq[i] * 0.15915494309189533577;
@@ -65,71 +61,46 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
         }
         __syncthreads();
     }
-    // channels kN c .. kN c + kN - 1: their angles, and for pairs (i, i + pairs) the lane that holds the other ones
-    const int lo = kN * c;
-    const bool turned = lo < 2 * a.pairs;
-    const bool second = lo >= a.pairs;
+    // channels lo .. lo + kN - 1: their angles, and for pairs (i, i + pairs) the lane that holds the other ones
+    const bool turned = lo < 2 * a.pairs, second = lo >= a.pairs;
     const int partner = (threadIdx.x & 48) + (second ? c - a.pairs / kN : c + a.pairs / kN);
     float cs[kN], sn[kN];
-    if (turned) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const float2 x = turn[a.interleaved ? (lo + i) / 2 : second ? lo + i - a.pairs : lo + i];
-            cs[i] = x.x;
-            sn[i] = (a.interleaved ? i % 2 == 0 : !second) ? -x.y : x.y;
-        }
+    for (int i = 0; i < kN; ++i) {
+        const float2 x = turned ? turn[a.interleaved ? (lo + i) / 2 : second ? lo + i - a.pairs : lo + i] : make_float2(1.f, 0.f);
+        cs[i] = x.x;
+        sn[i] = (a.interleaved ? i % 2 == 0 : !second) ? -x.y : x.y;
     }
-    for (int r = blockIdx.y * kGroups + group; r < rows; r += step) {
-        const int kind = r < a.Hq ? 0 : r < a.Hq + Hkv ? 1 : 2;           // q, k, v
-        const int h = kind == 0 ? r : kind == 1 ? r - a.Hq : r - a.Hq - Hkv;
-        const int n = a.fresh.len ? min(max(device_len(a.fresh, b, kind ? h : 0, Hkv), 0), a.T) : a.T;
-        char *q_to = kind == 0 ? a.q_out + (((size_t)b * a.Hq + h) * a.T + t) * (kD * kSize) + lo * kSize : nullptr;
-        float x[kN];
-        if (t >= n) {
-            if (kind == 0) {
-#pragma unroll
-                for (int i = 0; i < kN; ++i) x[i] = 0.f;
-                store_row<kN>(q_to, kBf16, x);
-            }
-            continue;
-        }
-        const RowsView &from = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-        load_row<kN>(from.base + b * from.batch + t * from.token + h * from.head + lo * kSize, kBf16, x);
-        const void *norm = kind == 0 ? a.q_norm : a.k_norm;
-        if (kind < 2 && norm) {
+    const int exchange = !a.pairs ? 0 : a.interleaved ? 1 : 2 * a.pairs == kD ? 2 : 3;
+
+    // Row r of the token: norm and rotation.
+    const auto form = [&](const RowsView &from, int h, const void *norm, float (&x)[kN]) {
+        load_row<kN, kBf16>(from.base + b * from.batch + t * from.token + h * from.head + lo * kSize, x);
+        if (norm) {
             float w[kN], sum = 0.f;
-            load_row<kN>((const char *)norm + lo * kSize, kBf16, w);
+            load_row<kN, kBf16>((const char *)norm + lo * kSize, w);
 #pragma unroll
             for (int i = 0; i < kN; ++i) sum = fmaf(x[i], x[i], sum);
             const float inv = 1.f / sqrtf(row16_reduce<SumOp>(sum) * (1.f / kD) + a.eps);
 #pragma unroll
             for (int i = 0; i < kN; ++i) x[i] = x[i] * inv * w[i];
         }
-        if (kind < 2 && a.pairs) {
-            float y[kN];
-            if (a.interleaved) {
+        if (exchange == 0) return;
+        float y[kN];
 #pragma unroll
-                for (int i = 0; i < kN; ++i) y[i] = x[i ^ 1];
-            } else {
+        for (int i = 0; i < kN; ++i) y[i] = exchange == 1 ? x[i ^ 1] : exchange == 2 ? dpp_pair<0x128>(x[i]) : __shfl(x[i], partner);
 #pragma unroll
-                for (int i = 0; i < kN; ++i) y[i] = __shfl(x[i], partner);
-            }
-            if (turned) {
-#pragma unroll
-                for (int i = 0; i < kN; ++i) x[i] = fmaf(x[i], cs[i], y[i] * sn[i]);
-            }
-        }
-        if (kind == 0) {
-            store_row<kN>(q_to, kBf16, x);
-            continue;
-        }
+        for (int i = 0; i < kN; ++i) x[i] = fmaf(x[i], cs[i], y[i] * sn[i]);
+    };
+    // A formed row of K or V to its place.
+    const auto store = [&](int h, int n, char *pages, uint8_t *scales, const float (&x)[kN]) {
         const int j = device_len(a.lens, b, h, Hkv) - n + t;
-        if (j < 0 || j >= a.cache.capacity) continue;                     // (a row that the cache has no room for)
+        if (j < 0 || j >= a.cache.capacity) return;                       // (a row that the cache has no room for)
         const int page = a.cache.table ? a.cache.table[(size_t)b * a.cache.pages_per_seq + (j >> a.cache.shift)] : b;
-        if (page < 0 || page >= a.cache.num_pages) continue;
+        if (page < 0 || page >= a.cache.num_pages) return;
         const size_t row = row_in_pool(a.cache, page, h, j);
         if constexpr (!kCodes) {
-            store_row<kN>((kind == 1 ? a.cache.k : a.cache.v) + row * (kD * kSize) + lo * kSize, kBf16, x);
+            store_row<kN, kBf16, kPast>(pages + row * (kD * kSize) + lo * kSize, x);
         } else {
             float top = 0.f;
 #pragma unroll
@@ -142,10 +113,30 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
             uint32_t w[kN / 4];
 #pragma unroll
             for (int i = 0; i < kN; i += 4) w[i / 4] = e4m3_codes(x[i] * inv, x[i + 1] * inv, x[i + 2] * inv, x[i + 3] * inv);
-            char *to = (kind == 1 ? a.cache.k : a.cache.v) + row * kD + lo;
-            if constexpr (kN == 8) *(u32x2 *)to = u32x2{w[0], w[1]};
-            else *(uint32_t *)to = w[0];
-            if (lo % kScaleBlock == 0) (kind == 1 ? a.cache.k_scale : a.cache.v_scale)[row * (kD / kScaleBlock) + lo / kScaleBlock] = (uint8_t)byte;
+            store_bytes<kN, kPast>(pages + row * kD + lo, w);
+            if (lo % kScaleBlock == 0) scales[row * (kD / kScaleBlock) + lo / kScaleBlock] = (uint8_t)byte;
+        }
+    };
+    for (int r = first; r < rows; r += step) {
+        const int g = r < a.Hq ? 0 : (r - a.Hq) % Hkv;
+        const int n = a.fresh.len ? min(max(device_len(a.fresh, b, g, Hkv), 0), a.T) : a.T;
+        float x[kN];
+        if (r < a.Hq) {
+            if (t < n) {
+                form(a.q, r, a.q_norm, x);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) x[i] = 0.f;
+            }
+            store_row<kN, kBf16, kPast>(a.q_out + (((size_t)b * a.Hq + r) * a.T + t) * (kD * kSize) + lo * kSize, x);
+        } else if (t >= n) {
+            continue;
+        } else if (r < a.Hq + Hkv) {
+            form(a.k, g, a.k_norm, x);
+            store(g, n, a.cache.k, a.cache.k_scale, x);
+        } else {
+            load_row<kN, kBf16>(a.v.base + b * a.v.batch + t * a.v.token + g * a.v.head + lo * kSize, x);
+            store(g, n, a.cache.v, a.cache.v_scale, x);
         }
     }
 }
@@ -175,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void read_rows(ReadArgs a, size_t total) 
         e4m3_values(w[0], s, x);
         e4m3_values(w[1], s, y);
         const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-        store_row<8>(to, kDtype == OBC_BF16, z);
+        store_row<8, kDtype == OBC_BF16, false>(to, z);
     } else {
 #pragma unroll
         for (int i = 0; i < kSize / 2; ++i) {
@@ -206,8 +197,11 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t stream) {
     const unsigned tokens = (unsigned)(a.B * a.T);
     const unsigned groups = (rows + kGroups - 1) / kGroups;
     const unsigned y = tokens < 1024 ? groups : 1;       // few tokens: every row a group of its own
+    // More than the eight dies' L2 hold is not read from them again.
+    const bool past = (size_t)tokens * rows * a.d * 2 > ((size_t)8 << 20);
     return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
-        append_rows<dim.value, type.value, codes.value><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
+        if (past) append_rows<dim.value, type.value, codes.value, true><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
+        else append_rows<dim.value, type.value, codes.value, false><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
         return hipGetLastError();
     });
 }
