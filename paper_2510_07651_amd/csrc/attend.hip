@@ -198,9 +198,11 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
         p->tile_rows = rows <= 16 ? 16 : 32;
         p->step = p->min_share = 128;
         // (us, 512 and 1024 workgroups: 64 x 8 heads x 1000 rows 42.5 and 49.6, 8 heads x 131072 101 and 105, 32 x 8 heads x 8192 ragged rows of
-        // 8 bits 70.9 and 72.5; shares of 128 and 256 tokens, 8 heads x 1025 8.4 and 9.8)
+        // 8 bits 70.9 and 72.5; shares of 128 and 256 tokens, 8 heads x 1025 8.4 and 9.8.  One share needs no second launch: in shares and
+        // in one 8 heads x 200 8.0 and 6.7, x 500 9.2 and 9.3, x 1025 8.6 and 14.6; 128 heads x 1025 19.1 and 17.7, x 2000 26.3 and 29.0;
+        // 256 heads x 2000 43.5 and 42.7.)
         want = 512;
-        least = 128;
+        least = capacity <= std::max(512LL, 10 * heads) ? capacity : 128;
     } else if (dtype == OBC_BF16) {
         // Two workgroups per compute unit.  A share costs its sums' way through memory, and one of few blocks its start (us, 32/8 heads: 512 rows over
         // 8192 in one share 101, in two 81; 1024 rows of 1024 in one 26.8, in two 33.3; 512 of 512 in one 16.4, in two 24.9; 16 over 8192
