@@ -136,6 +136,49 @@ def test_attend_scale_and_large_logits(dtype, kind):
     _run(dtype, kind, 1, 4, 2, 3, 128, 16, 8, [100], scale=1e-20)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("B,Hkv,G,T", [(3, 3, 2, 150), (5, 2, 1, 200), (3, 4, 2, 130), (1, 1, 8, 90), (24, 8, 1, 300)])
+def test_attend_many_heads_and_tiles(kind, B, Hkv, G, T):
+    """Heads that share dies evenly and not, more workgroups than run at once, tiles of all lengths."""
+    _run("bf16", kind, B, G * Hkv, Hkv, T, 64, 32, 10, [min(320, T + 11 * b) for b in range(B)], seed=B)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [1, 60])
+def test_attend_powers_of_two_of_all_sizes(dtype, T):
+    """8-bit values whose blocks' powers of two run from the least to large ones."""
+    cache, want = cu.make("e4m3", 1, 2, 128, 16, 8, seed=6)
+    e = torch.randint(10, 200, cache.v_scale.shape, generator=torch.Generator().manual_seed(1), dtype=torch.uint8)
+    cache.v_scale.copy_(e)
+    want["v"] = cu.held(cache)[1]
+    lens = torch.tensor([100], dtype=torch.int32)
+    q = torch.randn(1, 4, T, 128, generator=torch.Generator().manual_seed(2)).to(cu.DT[dtype])
+    out = obc.obc_attend(q.cuda(), cache, lens.cuda())
+    cu.check_attend(out, oc.attend(q, want, lens), 100, 128, dtype)
+
+
+def test_attend_replays_with_other_lengths():
+    """A chunk's call captured once, in several shares: lengths, queries and rows are read when it is replayed."""
+    for dtype, kind in TYPES:
+        cache, _ = cu.make(kind, 2, 2, 128, 64, 20, seed=3)
+        q = torch.zeros(2, 8, 40, 128, dtype=cu.DT[dtype], device="cuda")
+        lens, new = (torch.zeros(2, dtype=torch.int32, device="cuda") for _ in range(2))
+        out = torch.empty(2, 40, 8, 128, dtype=q.dtype, device="cuda")
+        ws = torch.empty(obc.obc_attend_workspace_bytes(2, 40, 8, cache, q.dtype), dtype=torch.uint8, device="cuda")
+        assert ws.numel() > 0
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            obc.obc_attend(q, cache, lens, new, out=out, workspace=ws)
+        for i, (ls, ns) in enumerate((([1280, 700], [40, 40]), ([40, 0], [40, 3]), ([555, 1279], [1, 39]))):
+            q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(i)))
+            lens.copy_(torch.tensor(ls))
+            new.copy_(torch.tensor(ns))
+            ws.fill_(255)
+            graph.replay()
+            assert torch.equal(obc.obc_attend(q, cache, lens, new), out)
+            torch.cuda.synchronize()
+
+
 def test_attend_pages_outside_the_pool():
     """They are read as the nearest page inside."""
     cache, _ = cu.make("bf16", 1, 2, 128, 16, 4, seed=2)
