@@ -155,6 +155,11 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, AttendPlan plan
     const int at = kManyRows ? blockIdx.x * kSlots + slot : blockIdx.x;
     if (kManyRows && at >= a.B * a.Hkv * rows) return;
     const int bg = at / rows, row = at % rows;
+    // The first record is on its way before the lengths say whether it counts: there is room for all of a plan's shares.
+    const int first = kManyRows ? 0 : slot;
+    const size_t rec_ahead = ((size_t)min(first, plan.splits - 1) * a.B * a.Hkv + bg) * rows + row;
+    const float2 ml_ahead = part_ml[rec_ahead];
+    const float4 o_ahead = *(const float4 *)(part_o + rec_ahead * kD + 4 * c);
     const Tile x = tile_of(a, bg, row / plan.tile_rows * plan.tile_rows, plan.tile_rows);
     const int share = share_of(x.seen, plan);
     const int shares = max((x.seen + share - 1) / share, 1);
@@ -166,7 +171,8 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, AttendPlan plan
         sum = sum * old + m.y * w;
         acc.x = acc.x * old + o.x * w; acc.y = acc.y * old + o.y * w; acc.z = acc.z * old + o.z * w; acc.w = acc.w * old + o.w * w;
     };
-    for (int s = kManyRows ? 0 : slot; s < shares; s += kManyRows ? 1 : kSlots) {
+    if (first < shares) add(ml_ahead, o_ahead);
+    for (int s = first + (kManyRows ? 1 : kSlots); s < shares; s += kManyRows ? 1 : kSlots) {
         const size_t rec = ((size_t)s * a.B * a.Hkv + bg) * rows + row;
         add(part_ml[rec], *(const float4 *)(part_o + rec * kD + 4 * c));
     }
