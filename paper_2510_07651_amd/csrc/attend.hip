@@ -195,10 +195,30 @@ size_t align_up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 
 }  // namespace
 
+// Shares per tile for attend_chunk, by the time that a call of full length would take.  A block of 32 tokens takes a workgroup 0.79 us (d = 64:
+// 0.54) alone on its compute unit and 1.05 (0.69) beside another; a round of workgroups starts in 4; joining takes 3 and its sums' way
+// to memory and back.  Predicted / measured, us, 32/8 heads: 512 rows over 8192 tokens in two shares 116 / 98, in four 89 / 83; 1024 of 1024
+// in one 29 / 27, in two 39 / 33; 256 over 2048 in four 27 / 29, in eight 30 / 30; four times 300 over 9000 in one 300 / 250, in three 235 / 217
+// (of ragged lengths 226 and 143), in four 256 / 235; 64 over 32768 in 16 65 / 57, in 32 56 / 54.
+static int chunk_shares(long long units, long long rows, int d, int capacity) {
+    const double alone = d == 128 ? 0.79 : 0.54, beside = d == 128 ? 1.05 : 0.69;
+    const int blocks = (capacity + 31) / 32;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 64 && (s == 1 || blocks / s >= 4); ++s) {
+        const long long n = units * s, left = n % 512;
+        const double rounds = (double)(n / 512) * beside + (left == 0 ? 0 : left <= 256 ? alone : beside);
+        const double t = rounds * ((blocks + s - 1) / s) + 4.0 * ((n + 511) / 512) + (s > 1 ? 3 + (double)rows * s * d * 1.8e-6 : 0);
+        if (s == 1 || t < least) { least = t; best = s; }
+        if (n > 4096) break;
+    }
+    return best;
+}
+
 void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, int cache_dtype, AttendPlan *p) {
     const long long rows = (long long)Hq / Hkv * T, heads = (long long)B * Hkv;
     *p = {};
-    long long want, least;              // workgroups (waves) that fill the chip, tokens of the shortest share
+    long long want = 1, least = 1;      // workgroups (waves) that fill the chip, tokens of the shortest share
     if (dtype == OBC_BF16 && rows <= 32) {
         p->form = kAttendToken;
         p->tile_rows = rows <= 16 ? 16 : 32;
@@ -210,16 +230,12 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
         want = 512;
         least = capacity <= std::max(512LL, 10 * heads) ? capacity : 128;
     } else if (dtype == OBC_BF16) {
-        // Two workgroups per compute unit.  A share costs its sums' way through memory, and one of few blocks its start (us, 32/8 heads: 512 rows over
-        // 8192 in one share 101, in two 81; 1024 rows of 1024 in one 26.8, in two 33.3; 512 of 512 in one 16.4, in two 24.9; 16 over 8192
-        // in shares of 1024 34.0, of 512 21.5, of 256 18.5; 256 over 2048 in shares of 512 28.7, of 256 30.4).
-        const long long units = heads * ((rows + kAttendChunkRows - 1) / kAttendChunkRows);
         p->form = kAttendChunk;
         p->tile_rows = kAttendChunkRows;
-        want = 512;
-        least = units >= 256 ? 2048 : units >= 64 ? 512 : 256;
         p->step = 32;
-        p->min_share = 256;
+        p->min_share = 128;
+        p->tiles = (int)((rows + kAttendChunkRows - 1) / kAttendChunkRows);
+        p->splits = chunk_shares(heads * p->tiles, heads * rows, d, capacity);
     } else {
         // One wave per SIMD, however short its share (us, 1024 waves and 2048: 4 x 8 heads x 8192 rows, G = 4, 55.5 and 64.1; 256 rows over 4096 172
         // and 185; shares of 32 and 128 tokens: 8 heads x 1000 rows 15.5 and 29.7).
@@ -229,8 +245,10 @@ void plan_attend(int B, int T, int Hq, int Hkv, int d, int capacity, int dtype, 
         want = 1024;
         least = 32;
     }
-    p->tiles = (int)((rows + p->tile_rows - 1) / p->tile_rows);
-    p->splits = (int)std::max(1LL, std::min(want / (heads * p->tiles), (capacity + least - 1) / least));
+    if (p->form != kAttendChunk) {
+        p->tiles = (int)((rows + p->tile_rows - 1) / p->tile_rows);
+        p->splits = (int)std::max(1LL, std::min(want / (heads * p->tiles), (capacity + least - 1) / least));
+    }
     if (p->splits > 1) {
         const size_t records = (size_t)p->splits * heads * rows;
         p->part_ml = 0;
