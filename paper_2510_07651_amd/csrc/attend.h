@@ -4,8 +4,6 @@
 // token by token: row r is token r / G of query head g G + r % G, and a tile of consecutive rows sees nearly the same tokens.
 #pragma once
 
-#include <type_traits>
-
 #include "cache.h"
 
 namespace obc {
@@ -49,20 +47,6 @@ __device__ __forceinline__ void store4(void *p, const float (&x)[4]) {
     } else {
         store_bytes<16, false>(p, x);
     }
-}
-
-// Calls `f` with a kernel's compile-time choices.
-template <typename F>
-hipError_t with_types(int d, int dtype, int cache_dtype, F &&f) {
-    const bool codes = cache_dtype == OBC_E4M3;
-    using std::integral_constant;
-    const auto by_codes = [&](auto dim, auto type) {
-        return codes ? f(dim, type, std::true_type()) : f(dim, type, std::false_type());
-    };
-    const auto by_type = [&](auto dim) {
-        return dtype == OBC_BF16 ? by_codes(dim, integral_constant<int, OBC_BF16>()) : by_codes(dim, integral_constant<int, OBC_F32>());
-    };
-    return d == 128 ? by_type(integral_constant<int, 128>()) : by_type(integral_constant<int, 64>());
 }
 
 hipError_t launch_attend_token(const AttendArgs &a, const AttendPlan &p, float2 *part_ml, float *part_o, hipStream_t stream);

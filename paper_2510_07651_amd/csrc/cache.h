@@ -2,6 +2,8 @@
 // Internal to the library.
 #pragma once
 
+#include <type_traits>
+
 #include "internal.h"
 
 namespace obc {
@@ -160,6 +162,20 @@ struct AttendPlan {
     int step, min_share;     // a share: a multiple of `step` tokens, at least `min_share`
     size_t part_ml, part_o, total;
 };
+
+// Calls `f` with a kernel's compile-time choices.
+template <typename F>
+hipError_t with_types(int d, int dtype, int cache_dtype, F &&f) {
+    const bool codes = cache_dtype == OBC_E4M3;
+    using std::integral_constant;
+    const auto by_codes = [&](auto dim, auto type) {
+        return codes ? f(dim, type, std::true_type()) : f(dim, type, std::false_type());
+    };
+    const auto by_type = [&](auto dim) {
+        return dtype == OBC_BF16 ? by_codes(dim, integral_constant<int, OBC_BF16>()) : by_codes(dim, integral_constant<int, OBC_F32>());
+    };
+    return d == 128 ? by_type(integral_constant<int, 128>()) : by_type(integral_constant<int, 64>());
+}
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t stream);
 hipError_t launch_cache_read(const ReadArgs &a, hipStream_t stream);

@@ -148,7 +148,7 @@ int obc_cache_read(const obc_cache_t *cache, const int32_t *keep_idx, void *k_ou
     if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(keep_idx, 4)) return OBC_EINVAL;
     if (dtype != OBC_F32 && dtype != OBC_BF16) return OBC_EUNSUPPORTED;
     if (cache->dtype != dtype && cache->dtype != OBC_E4M3) return OBC_EUNSUPPORTED;
-    if ((long long)B * cache->Hkv * n > (1LL << 34)) return OBC_EUNSUPPORTED;
+    if (n > OBC_MAX_CACHE_ROWS / 8 || (long long)B * cache->Hkv * n > (1LL << 34)) return OBC_EUNSUPPORTED;
     a.keep = keep_idx;
     a.k_out = (char *)k_out;
     a.v_out = (char *)v_out;

@@ -121,7 +121,7 @@ def test_attend_refusals(lib):
 
 def test_read_refusals(lib):
     bad = [(dict(k_out=None), obc.OBC_EINVAL), (dict(v_out=None), obc.OBC_EINVAL), (dict(k_out=FAKE + 8), obc.OBC_EINVAL), (dict(B=1), obc.OBC_EINVAL),
-           (dict(n=0), obc.OBC_EINVAL), (dict(n=65), obc.OBC_EINVAL), (dict(keep=FAKE + 2), obc.OBC_EINVAL), (dict(dtype=obc.OBC_F32), obc.OBC_EUNSUPPORTED),
+           (dict(n=0), obc.OBC_EINVAL), (dict(n=65), obc.OBC_EINVAL), (dict(n=(1 << 27) + 1, keep=FAKE), obc.OBC_EUNSUPPORTED), (dict(keep=FAKE + 2), obc.OBC_EINVAL), (dict(dtype=obc.OBC_F32), obc.OBC_EUNSUPPORTED),
            (dict(dtype=obc.OBC_E4M3), obc.OBC_EUNSUPPORTED)]
     for change, status in bad:
         assert _read(lib, **change) == status, change

@@ -147,6 +147,19 @@ def test_read(kind, dtype, d):
                 assert x.dtype is cu.DT[dtype] and torch.equal(x.double().cpu(), ref)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_read_many_rows(dtype):
+    """Enough rows for a thread to take 16 codes; the numbers of rows and heads are no multiples of anything."""
+    cache, _ = cu.make("e4m3", 3, 5, 64, 16, 560, seed=5)
+    keep = torch.randint(-1, cache.capacity, (3, 5, 8801), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    got = obc.obc_cache_read(cache, keep_idx=keep.cuda(), dtype=cu.DT[dtype])
+    table = cache.page_table.cpu().long()
+    at = torch.gather(table[:, None].expand(3, 5, -1), 2, keep.clamp(min=0).long() // 16)
+    for x, held in zip(got, cu.held(cache)):
+        want = held[at, torch.arange(5)[:, None], keep.clamp(min=0).long() % 16] * (keep >= 0)[..., None]
+        assert torch.equal(x.double().cpu(), want)
+
+
 def test_rows_keep_their_values_when_stored_again():
     """e4m3 rows read back and stored again: the same values, whatever power of two the new block takes."""
     g = torch.Generator().manual_seed(9)
