@@ -37,6 +37,52 @@ __device__ __forceinline__ void store_row(char *p, const float (&x)[kN]) {
     }
 }
 
+// Row `j` of head h of sequence b (a row that the cache has no room for is dropped): this lane's kN channels from lo on.  A block of 32
+// channels lies in 4 lanes (8 of half as many), which find its power of two together.
+template <int kN, bool kBf16, bool kCodes, bool kPast>
+__device__ __forceinline__ void put_row(const CacheView &c, char *pages, uint8_t *scales, int b, int h, long long at, int lo, const float (&x)[kN]) {
+    constexpr int kD = 16 * kN, kSize = kBf16 ? 2 : 4;
+    if (at < 0 || at >= c.capacity) return;
+    const int j = (int)at, page = c.table ? c.table[(size_t)b * c.pages_per_seq + (j >> c.shift)] : b;
+    if (page < 0 || page >= c.num_pages) return;
+    const size_t row = row_in_pool(c, page, h, j);
+    if constexpr (!kCodes) {
+        store_row<kN, kBf16, kPast>(pages + row * (kD * kSize) + lo * kSize, x);
+    } else {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) top = fmaxf(top, finite_abs(x[i]));
+        top = fmaxf(top, dpp_pair<0xB1>(top));
+        top = fmaxf(top, dpp_pair<0x4E>(top));
+        if constexpr (kN == 4) top = fmaxf(top, dpp_pair<0x141>(top));
+        const uint32_t byte = scale_byte(top);
+        const float inv = scale_inverse(byte);
+        uint32_t w[kN / 4];
+#pragma unroll
+        for (int i = 0; i < kN; i += 4) w[i / 4] = e4m3_codes(x[i] * inv, x[i + 1] * inv, x[i + 2] * inv, x[i + 3] * inv);
+        store_bytes<kN, kPast>(pages + row * kD + lo, w);
+        if (lo % kScaleBlock == 0) scales[row * (kD / kScaleBlock) + lo / kScaleBlock] = (uint8_t)byte;
+    }
+}
+
+// Rows that are stored as they are: 16 of a head per workgroup, so that neighbours in a page (and their scale bytes) are written together; K
+// and V in one launch.
+template <int kD, int kDtype, bool kCodes, bool kPast>
+__global__ __launch_bounds__(kThreads) void store_rows(AppendArgs a) {
+    constexpr int kN = kD / 16, kSize = kDtype == OBC_BF16 ? 2 : 4;
+    const int t = blockIdx.x * kGroups + threadIdx.x / 16, lo = threadIdx.x % 16 * kN;
+    const int b = blockIdx.y / a.cache.Hkv, g = blockIdx.y % a.cache.Hkv;
+    const int n = a.fresh.len ? min(max(device_len(a.fresh, b, g, a.cache.Hkv), 0), a.T) : a.T;
+    if (t >= n) return;
+    const RowsView &from = blockIdx.z == 0 ? a.k : a.v;
+    Raw<kN, kDtype == OBC_BF16> raw;
+    load_bytes<kN * kSize>(raw.w, from.base + b * from.batch + t * from.token + g * from.head + lo * kSize);
+    float x[kN];
+    widen<kN, kDtype == OBC_BF16>(raw, x);
+    put_row<kN, kDtype == OBC_BF16, kCodes, kPast>(a.cache, blockIdx.z == 0 ? a.cache.k : a.cache.v, blockIdx.z == 0 ? a.cache.k_scale : a.cache.v_scale,
+                                                   b, g, (long long)device_len(a.lens, b, g, a.cache.Hkv) - n + t, lo, x);
+}
+
 // One workgroup per new token (and per 16 * gridDim.y of its heads): a row of d channels lies in 16 lanes, so the sum of its
 // squares is four lane exchanges, and a lane keeps its channels' norm weights, cosines and sines for all heads of the token.
 // The angle pos * f is reduced to a part of one turn in 64 bits: in fp32 the product alone would be off by 2^-24 of the angle,
@@ -111,31 +157,8 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) x[i] = fmaf(x[i], cs[i], y[i] * sn[i]);
     };
-    // A formed row of K or V to its place.
     const auto store = [&](int h, int n, char *pages, uint8_t *scales, const float (&x)[kN]) {
-        const long long at = (long long)device_len(a.lens, b, h, Hkv) - n + t;
-        if (at < 0 || at >= a.cache.capacity) return;                     // (a row that the cache has no room for)
-        const int j = (int)at;
-        const int page = a.cache.table ? a.cache.table[(size_t)b * a.cache.pages_per_seq + (j >> a.cache.shift)] : b;
-        if (page < 0 || page >= a.cache.num_pages) return;
-        const size_t row = row_in_pool(a.cache, page, h, j);
-        if constexpr (!kCodes) {
-            store_row<kN, kBf16, kPast>(pages + row * (kD * kSize) + lo * kSize, x);
-        } else {
-            float top = 0.f;
-#pragma unroll
-            for (int i = 0; i < kN; ++i) top = fmaxf(top, finite_abs(x[i]));
-            top = fmaxf(top, dpp_pair<0xB1>(top));                        // the block's lanes: 4, or 8 of half as many channels
-            top = fmaxf(top, dpp_pair<0x4E>(top));
-            if constexpr (kN == 4) top = fmaxf(top, dpp_pair<0x141>(top));
-            const uint32_t byte = scale_byte(top);
-            const float inv = scale_inverse(byte);
-            uint32_t w[kN / 4];
-#pragma unroll
-            for (int i = 0; i < kN; i += 4) w[i / 4] = e4m3_codes(x[i] * inv, x[i + 1] * inv, x[i + 2] * inv, x[i + 3] * inv);
-            store_bytes<kN, kPast>(pages + row * kD + lo, w);
-            if (lo % kScaleBlock == 0) scales[row * (kD / kScaleBlock) + lo / kScaleBlock] = (uint8_t)byte;
-        }
+        put_row<kN, kBf16, kCodes, kPast>(a.cache, pages, scales, b, h, (long long)device_len(a.lens, b, h, Hkv) - n + t, lo, x);
     };
     for (int r = first; r < rows; r += step) {
         const int g = r < a.Hq ? 0 : r < a.Hq + Hkv ? r - a.Hq : r - a.Hq - Hkv;
@@ -216,6 +239,14 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t stream) {
     const unsigned y = tokens < 1024 ? groups : 1;       // few tokens: every row a group of its own
     // More than the eight dies' L2 hold is not read from them again.
     const bool past = (size_t)tokens * rows * a.d * 2 > ((size_t)8 << 20);
+    if (!a.Hq && !a.pairs && !a.k_norm) {
+        const dim3 grid((a.T + kGroups - 1) / kGroups, a.B * a.cache.Hkv, 2);
+        return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
+            if (past) store_rows<dim.value, type.value, codes.value, true><<<grid, kThreads, 0, stream>>>(a);
+            else store_rows<dim.value, type.value, codes.value, false><<<grid, kThreads, 0, stream>>>(a);
+            return hipGetLastError();
+        });
+    }
     return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
         if (past) append_rows<dim.value, type.value, codes.value, true><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
         else append_rows<dim.value, type.value, codes.value, false><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
