@@ -364,7 +364,8 @@ typedef struct {
  * Rows t >= n_b are not written to the cache and are zero in q_out.
  * q may be NULL (with q_out, q_norm NULL and Hq 0): rows that are stored as they are, such as those an eviction kept; only then
  * may new_lens be [B, Hkv] (new_lens_per_head = 1: the lists of obc_select_adaptive).
- * `dtype` (OBC_F32 or OBC_BF16) is the inputs'; the cache's is the same or OBC_E4M3.
+ * `dtype` (OBC_F32 or OBC_BF16) is the inputs'; the cache's is the same or OBC_E4M3.  q_out and the cache must not overlap the
+ * inputs.  B * T < 2^24; 2^27 for rows that are stored as they are.
  */
 int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t *v, const obc_cache_t *cache, void *q_out,
                      const int32_t *lens, int lens_per_head, const int32_t *new_lens, int new_lens_per_head,

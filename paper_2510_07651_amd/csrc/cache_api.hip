@@ -92,7 +92,10 @@ int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t 
         !aligned(k_norm, 16))
         return OBC_EINVAL;
     if ((q_norm || k_norm) && !(eps >= 0.f && std::isfinite(eps))) return OBC_EINVAL;
-    if ((long long)B * T > (1LL << 28) || (long long)B * T * (Hq + 2LL * cache->Hkv) > (1LL << 34) || Hq > 65535) return OBC_EUNSUPPORTED;
+    // A grid holds fewer than 2^32 threads: with norm, rotation or queries a workgroup of 256 per token, else one per 16 rows.
+    const bool as_they_are = !q && !rot_pairs && !k_norm;
+    if ((long long)B * T >= (as_they_are ? 1LL << 27 : 1LL << 24) || (long long)B * T * (Hq + 2LL * cache->Hkv) > (1LL << 34) || Hq > 65535)
+        return OBC_EUNSUPPORTED;
     a.q_out = (char *)q_out;
     a.lens = {lens, lens_per_head != 0};
     a.fresh = {new_lens, new_lens_per_head != 0};

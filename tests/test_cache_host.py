@@ -98,6 +98,12 @@ def test_append_refusals(lib):
     assert _append(lib, _cache(dtype=obc.OBC_F32)) == obc.OBC_EUNSUPPORTED
 
 
+@pytest.mark.parametrize("change", [dict(q=_rows(), q_out=FAKE, Hq=2), dict(pairs=64, pos=FAKE, freq=FAKE), dict(k_norm=FAKE)])
+def test_append_refuses_more_tokens_than_a_grid_holds(lib, change):
+    assert _append(lib, T=1 << 23, **change) == obc.OBC_EUNSUPPORTED          # 2 sequences: 2^24 workgroups of 2^8 threads
+    assert _append(lib, T=1 << 26) == obc.OBC_EUNSUPPORTED
+
+
 def test_attend_refusals(lib):
     bad = [
         (dict(q=None), obc.OBC_EINVAL), (dict(out=None), obc.OBC_EINVAL), (dict(lens=None), obc.OBC_EINVAL), (dict(q=FAKE + 8), obc.OBC_EINVAL),
