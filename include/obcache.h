@@ -322,7 +322,8 @@ int obc_compact_scores(const float *scores, const int32_t *keep_idx, float *scor
  *               channels of a row, whose values are code * 2^e, the codes 8-bit floating-point numbers of four
  *               exponent and three mantissa bits (no infinities, largest 448).  e is the least integer for which no finite value
  *               of the block exceeds 448 * 2^e, at least -117; codes are rounded to nearest even; infinities and NaN become
- *               NaN.  Every stored value is exact in bf16, and a row read back and stored again keeps its values.
+ *               NaN.  Every stored value is exact in bf16, and a row read back and stored again keeps its values.  (Values from
+ *               31/32 * 2^128 on round to 2^128 and are read back as infinity, as bf16 does a little below its range's end.)
  * Alignment: k, v and scales 16 bytes, tables 4.  pages_per_seq * page_size <= OBC_MAX_CACHE_ROWS, batch * Hkv <= 65535.
  * Page numbers are device data that is not checked on the host: a number outside the pool is taken as the nearest inside by calls
  * that read, and rows that would be written there are dropped.  Several sequences may read one page; what a

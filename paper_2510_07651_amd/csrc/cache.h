@@ -44,7 +44,8 @@ __device__ __forceinline__ size_t row_in_pool(const CacheView &c, int page, int 
 // The stored byte is e + 127 with e the least integer for which absmax <= 448 * 2^e (absmax of the block's finite values), at
 // least -117, so that every value a code stands for is a normal fp32 (and bf16) number: 2^-9 * 2^-117 = 2^-126.  448 = 1.75 * 2^8.
 // Dividing by 2^e is exact and multiplying back is too, in bf16 as well (four significant bits): the only rounding is the one
-// to the code, and rows that are read back and stored again keep their values.
+// to the code, and rows that are read back and stored again keep their values.  (Only values that round to 2^128 have no place in fp32: they
+// are read back as infinity.)
 constexpr int kScaleBlock = 32;
 constexpr uint32_t kLeastScale = 10;
 __device__ __forceinline__ uint32_t scale_byte(float absmax) {

@@ -87,6 +87,9 @@ __global__ __launch_bounds__(kThreads) void store_rows(AppendArgs a) {
 // squares is four lane exchanges, and a lane keeps its channels' norm weights, cosines and sines for all heads of the token.
 // The angle pos * f is reduced to a part of one turn in 64 bits: in fp32 the product alone would be off by 2^-24 of the angle,
 // 0.06 rad at a million tokens.
+//
+// Bound by HBM, with the vector work beside it: 8192 tokens of 32/8 heads in bf16 (201 MB) 48 us; without norm and rotation 38.5, a copy of as many
+// bytes 39.0.  A single token: 3.4 us, the launch and its trips to memory.
 template <int kD, int kDtype, bool kCodes, bool kPast>
 __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
     constexpr int kN = kD / 16;

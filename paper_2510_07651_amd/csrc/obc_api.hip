@@ -102,7 +102,7 @@ using namespace obc;
 
 extern "C" {
 
-int obc_version(void) { return 104; }
+int obc_version(void) { return 105; }
 
 int obc_init(void) {
     void *p = nullptr;

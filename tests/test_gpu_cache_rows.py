@@ -131,6 +131,19 @@ def test_codes_of_special_values():
             assert torch.equal(torch.nan_to_num(got, nan=12345.0), torch.nan_to_num(values, nan=12345.0))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_codes_at_the_end_of_the_range(dtype):
+    """Below 31/32 * 2^128 values keep to half a step; from there on the nearest code stands for 2^128."""
+    inside, outside = 30 / 32 * 2.0 ** 128, 31 / 32 * 2.0 ** 128           # (both are fp32 and bf16 numbers)
+    x = torch.zeros(1, 1, 1, 64)
+    x[..., 0], x[..., 32], x[..., 33] = inside, outside, -outside
+    cache, _ = cu.make("e4m3", 1, 1, 64, 8, 0)
+    obc.obc_cache_append(cache, x.to(cu.DT[dtype]).cuda(), x.to(cu.DT[dtype]).cuda(), torch.tensor([1], dtype=torch.int32, device="cuda"))
+    for out in (torch.float32, torch.bfloat16):
+        got = obc.obc_cache_read(cache, 1, dtype=out)[0][0, 0, 0].cpu()
+        assert got[0] == inside and got[32] == math.inf and got[33] == -math.inf and int((got == 0).sum()) == 61
+
+
 @pytest.mark.parametrize("kind,dtype", [("bf16", "bf16"), ("fp32", "fp32"), ("e4m3", "bf16"), ("e4m3", "fp32")])
 @pytest.mark.parametrize("d", [64, 128])
 def test_read(kind, dtype, d):
