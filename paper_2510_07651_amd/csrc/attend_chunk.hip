@@ -28,6 +28,9 @@ __device__ __forceinline__ int value_slot(int R, int c) { return kD == 128 ? (c 
 template <int kD>
 __device__ __forceinline__ int value_piece(int R, int slot) { return kD == 128 ? (slot - 4 * (R & 3)) & 15 : (slot - 4 * ((R >> 1) & 1)) & 7; }
 
+// Groups that the eight dies are parted into, one per residue of the KV head.
+__host__ __device__ constexpr int die_classes(int Hkv) { return Hkv % 8 == 0 ? 8 : Hkv % 4 == 0 ? 4 : Hkv % 2 == 0 ? 2 : 1; }
+
 typedef const __attribute__((address_space(4))) int32_t *table_ptr;    // read through scalar loads
 
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -173,10 +176,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, Attend
     __shared__ __attribute__((aligned(1024))) char smem[kRing * S::kSlot];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
 
-    // Which tile: workgroups go to the eight dies in turn; those of one KV head stay on as few as there are heads for, so that they
-    // find its rows in that die's L2.  Late tiles, which see most, first (2048 rows of a prompt of 2048, 32/8 heads: 56.1 us, with those that share a
+    // Which tile: workgroups go to the eight dies in turn; those of KV head g, of all sequences, stay on as few as there are KV heads for, so that
+    // they find its rows in that die's L2 and every die has its part of the long sequences and of the short ones (us, with the dies dealt by
+    // sequence and KV head, and so: 4 x 512 rows over at most 8192, 16/2 heads 155 and 124, 8 x 256, 8/1 heads 82 and 66; all of one length 170 and
+    // 171, 94 and 95).  Late tiles, which see most, first (2048 rows of a prompt of 2048, 32/8 heads: 56.1 us, with those that share a
     // compute unit folded 50.9; 1500 over 4000 106.0, 103.7).
-    const int heads = a.B * a.Hkv, die = blockIdx.x & 7, classes = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
+    const int heads = a.B * a.Hkv, die = blockIdx.x & 7, classes = die_classes(a.Hkv);
     const int per_head = plan.tiles * plan.splits, line = (per_head + 8 / classes - 1) / (8 / classes), mine = heads / classes;
     const int at = (int)(blockIdx.x >> 3);
     int head = at / line, in_line = at % line;
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, Attend
 }  // namespace
 
 hipError_t launch_attend_chunk(const AttendArgs &a, const AttendPlan &p, float2 *part_ml, float *part_o, hipStream_t stream) {
-    const int heads = a.B * a.Hkv, classes = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
+    const int heads = a.B * a.Hkv, classes = die_classes(a.Hkv);
     const long long per_head = (long long)p.tiles * p.splits, line = (per_head + 8 / classes - 1) / (8 / classes);
     const dim3 grid((unsigned)(8 * line * (heads / classes)));
     return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto, auto codes) {
