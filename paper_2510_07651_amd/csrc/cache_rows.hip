@@ -157,8 +157,9 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
         float y[kN];
 #pragma unroll
         for (int i = 0; i < kN; ++i) y[i] = exchange == 1 ? x[i ^ 1] : exchange == 2 ? dpp_pair<0x128>(x[i]) : __shfl(x[i], partner);
+        // (a selection, no angle of 0: 0 times another lane's infinity is no 0)
 #pragma unroll
-        for (int i = 0; i < kN; ++i) x[i] = fmaf(x[i], cs[i], y[i] * sn[i]);
+        for (int i = 0; i < kN; ++i) x[i] = turned ? fmaf(x[i], cs[i], y[i] * sn[i]) : x[i];
     };
     const auto store = [&](int h, int n, char *pages, uint8_t *scales, const float (&x)[kN]) {
         put_row<kN, kBf16, kCodes, kPast>(a.cache, pages, scales, b, h, (long long)device_len(a.lens, b, h, Hkv) - n + t, lo, x);

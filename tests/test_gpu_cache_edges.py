@@ -1,0 +1,69 @@
+"""The cache calls where their definitions are easy to miss: values that are not finite, the cache's end, the ends of the number ranges."""
+import math
+
+import pytest
+import torch
+
+from oracle import cache as oc
+from paper_2510_07651_amd import binding as obc
+
+import cache_util as cu
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [("bf16", "bf16"), ("bf16", "e4m3"), ("fp32", "fp32"), ("fp32", "e4m3")]
+
+
+def _i32(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _bits(x):
+    return x.contiguous().view(torch.int16 if x.dtype is torch.bfloat16 else torch.int32)
+
+
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("d,pairs", [(64, 8), (64, 16), (128, 16), (128, 32), (128, 56)])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "neighbours"])
+def test_channels_that_are_not_turned_stay_as_they_are(dtype, kind, d, pairs, interleaved):
+    """An infinity, a NaN and a negative zero, in channels that are turned and in others: nothing reaches a channel from 2 * pairs on, and of
+    the turned ones only the other of the pair."""
+    B, T, Hq, Hkv = 1, 9, 4, 2
+    g = torch.Generator().manual_seed(d + pairs)
+    rows = torch.randn(B, T, Hq + Hkv, d, generator=g)
+    turned = 2 * pairs
+    rows[:, :, :, turned::5] = -0.0
+    at = {1: 3, 2: 3, 3: turned - 2, 4: pairs, 5: turned, 6: d - 1, 7: 0}
+    for t, c in at.items():
+        rows[:, t, :, c] = (math.inf, math.nan, -math.inf)[t % 3]
+    rows[:, 8] = -0.0
+    rows = rows.to(cu.DT[dtype])
+    q, k = rows[:, :, :Hq], rows[:, :, Hq:]
+    cache, _ = cu.make(kind, B, Hkv, d, 16, 1, seed=1)
+    page = int(cache.page_table[0, 0])
+    freq = cu.rotation(pairs)
+    pos = torch.randint(1, 5000, (B, T), generator=g, dtype=torch.int32)
+    got = obc.obc_cache_append(cache, k.cuda(), k.cuda(), _i32(T), q=q.cuda(), positions=pos.cuda(), inv_freq=freq.cuda(), interleaved=interleaved)
+    torch.cuda.synchronize()
+    assert torch.equal(_bits(got.transpose(1, 2)[..., turned:].cpu()), _bits(q[..., turned:]))
+    if kind != "e4m3":
+        assert torch.equal(_bits(cache.k[page, :, :T, turned:].cpu().transpose(0, 1)), _bits(k[0, ..., turned:]))
+    held = cu.held(cache)[0][page]
+    slack = cu.append_slack(torch.nan_to_num(rows.double(), nan=0.0, posinf=0.0, neginf=0.0), None, 1.0)
+    for t in range(T):
+        c = at.get(t, d)
+        other = d if c >= turned else (c ^ 1 if interleaved else (c + pairs) % turned)
+        fine = torch.tensor([i not in (c, other) for i in range(d)])
+        for h in range(Hq + Hkv):
+            want = oc.turned(rows[0, t, h].double(), None, 0, pos[0, t], freq, 1.0, interleaved)
+            if h < Hq:
+                cu.close(got[0, h, t].cpu()[fine], want[fine], dtype, slack[0, t, h][fine])
+            elif kind != "e4m3":
+                cu.close(held[h - Hq, t][fine], want[fine], kind, slack[0, t, h][fine])
+            else:
+                # blocks without a turned channel: the codes of these very values
+                for i in range(0, d, 32):
+                    if i >= turned:
+                        codes, byte = oc.e4m3(rows[0, t, h, i:i + 32].double())
+                        assert torch.equal(torch.nan_to_num(held[h - Hq, t, i:i + 32], nan=1e9), torch.nan_to_num(codes, nan=1e9))
+                        assert int(cache.k_scale[page, h - Hq, t, i // 32]) == int(byte)
