@@ -377,12 +377,14 @@ int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t 
  * Attention of the new rows over the cache:
  *   out[b,t,h,:] = sum_j p_j v_j,  p = softmax_j(scale * q[b,h,t].k_j)
  * over the rows j < lens - n_b + t + 1 of KV head h / (Hq/Hkv) (causal = 1: a new row sees what was there and the new
- * rows up to itself), or over all j < lens (causal = 0: cross attention).  T = 1 is a decoding step, a larger T a chunk of a prompt.
+ * rows up to itself), or over all j < lens (causal = 0: cross attention), those of them that the cache has: where lens is larger than
+ * pages_per_seq * page_size the last new rows have no place (obc_cache_append drops them) and the others see what they would see otherwise.
+ * A negative lens counts as 0.  T = 1 is a decoding step, a larger T a chunk of a prompt.
  *   q    [B, Hq, T, d] of `dtype` (OBC_F32 or OBC_BF16); the cache is of the same type or OBC_E4M3
  *   out  [B, T, Hq, d] of `dtype` (what the output projection takes), written in full: rows t >= n_b, and rows that see
  *        nothing, are 0.  Must not alias the inputs.
- * lens is brought into [0, pages_per_seq * page_size].  Rows of the cache from lens on, pages that only hold such rows, and rows
- * t >= n_b of q may hold anything; NaN or an infinity in the first `lens` rows gives undefined results for that KV head.
+ * Rows of the cache from lens on, pages that only hold such rows, and rows t >= n_b of q may hold anything; NaN or an infinity in the
+ * first `lens` rows gives undefined results for that KV head.
  * Products are summed in fp32.  With bf16 queries the weights are rounded to bf16 before they meet v.
  * scale > 0 (1/sqrt(d) is the usual one).  workspace: obc_attend_workspace_bytes(...) bytes, 256-byte aligned (none needed where
  * that is 0).  Calls that may run at the same time need workspaces of their own.

@@ -109,12 +109,12 @@ def attend(q, cache, lens, new_lens=None, causal=True, scale=None):
     for b in range(B):
         n = T if new_lens is None else min(max(int(new_lens[b]), 0), T)
         for g in range(Hkv):
-            x = min(max(length(lens, b, g), 0), capacity(cache))
-            at = [place(cache, b, g, j) for j in range(x)]
+            x, cap = max(length(lens, b, g), 0), capacity(cache)
+            at = [place(cache, b, g, j) for j in range(min(x, cap))]
             k = torch.stack([cache["k"][i] for i in at]) if at else torch.zeros(0, d, dtype=torch.float64)
             v = torch.stack([cache["v"][i] for i in at]) if at else k
             for t in range(n):
-                seen = max(x - n + t + 1, 0) if causal else x
+                seen = min(max(x - n + t + 1, 0) if causal else x, cap)      # (its own row is row x - n + t, within the cache or past it)
                 if seen == 0:
                     continue
                 for h in range(g * (Hq // Hkv), (g + 1) * (Hq // Hkv)):

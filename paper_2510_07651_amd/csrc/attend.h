@@ -12,24 +12,23 @@ constexpr int kAttendChunkRows = 128;  // rows per workgroup of attend_chunk
 constexpr float kLazy = 8.f;           // log2 of how far a weight may grow past its reference before sums are rescaled
 constexpr float kNone = -3.0e38f;      // running maximum of a row that has seen nothing: finite, so that differences stay numbers
 
-// Tokens the rows of new token t see of a KV head with `len` rows, `n` of them new.
-__device__ __forceinline__ int tokens_seen(int len, int n, int t, int causal) {
-    if (t >= n) return 0;
-    return causal ? max(len - n + t + 1, 0) : len;
-}
-
 struct Tile {            // rows r0 .. r0 + size - 1 of KV head g of sequence b
-    int b, g, r0, len, n, seen;      // seen: the most any of its rows sees
+    int b, g, r0, len, n, seen;      // len: rows of the KV head, also those for which the cache had no room; n: new tokens; seen: the most any row sees
+    // Tokens that the rows of new token t see, if the cache had room for all: the token's own row is row len - n + t.
+    __device__ __forceinline__ int sees(int t, int causal) const {
+        if (t >= n) return 0;
+        return causal ? max(len - n + t + 1, 0) : len;
+    }
 };
 __device__ __forceinline__ Tile tile_of(const AttendArgs &a, int bg, int r0, int size) {
     Tile x;
     x.b = bg / a.Hkv;
     x.g = bg % a.Hkv;
     x.r0 = r0;
-    x.len = min(max(device_len(a.lens, x.b, x.g, a.Hkv), 0), a.cache.capacity);
+    x.len = min(max(device_len(a.lens, x.b, x.g, a.Hkv), 0), a.cache.capacity + a.T);    // (from there on every new token sees the whole cache)
     x.n = a.fresh ? min(max(a.fresh[x.b], 0), a.T) : a.T;
     const int first = r0 / a.G, last = min((r0 + size - 1) / a.G, x.n - 1);
-    x.seen = first <= last ? tokens_seen(x.len, x.n, last, a.causal) : 0;
+    x.seen = first <= last ? min(x.sees(last, a.causal), a.cache.capacity) : 0;
     return x;
 }
 // Tokens per share of a tile: the same in the kernels that leave partial sums and in the one that joins them.  A sequence that is short

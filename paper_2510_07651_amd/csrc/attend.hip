@@ -31,8 +31,8 @@ __global__ __launch_bounds__(256, 1) void attend_fp32(AttendArgs a, AttendPlan p
 
     const int row = x.r0 + col, t = row / a.G, h = x.g * a.G + row % a.G;
     const bool exists = t < a.T;
-    const int seen = exists ? min(tokens_seen(x.len, x.n, t, a.causal), end) : 0;
-    const int full = x.r0 / a.G < x.n ? min(tokens_seen(x.len, x.n, x.r0 / a.G, a.causal), end) : 0;
+    const int seen = exists ? min(x.sees(t, a.causal), end) : 0;
+    const int full = x.r0 / a.G < x.n ? min(x.sees(x.r0 / a.G, a.causal), end) : 0;
     float4 q[kD / 8];             // channels 8 s + 4 half ..
     const char *q_row = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * (kD * 4) + 16 * half;
 #pragma unroll

@@ -201,8 +201,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, Attend
 
     const int r0 = x.r0 + wave * 32, row = r0 + col, t = row / a.G, h = x.g * a.G + row % a.G;
     const bool exists = t < a.T;
-    const int seen = exists ? min(tokens_seen(x.len, x.n, t, a.causal), end) : 0;
-    const int full = r0 / a.G < x.n ? min(tokens_seen(x.len, x.n, r0 / a.G, a.causal), end) : 0;    // tokens that every row that counts sees
+    const int seen = exists ? min(x.sees(t, a.causal), end) : 0;
+    const int full = r0 / a.G < x.n ? min(x.sees(r0 / a.G, a.causal), end) : 0;    // tokens that every row that counts sees
     bf16x8 q[S::kSteps];
     const char *q_row = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * S::kRow + half * 16;
 #pragma unroll

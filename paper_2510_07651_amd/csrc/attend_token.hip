@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_token(AttendArgs a, Attend
     for (int s = 0; s < kSets; ++s) {
         const int row = 16 * s + col, t = row / a.G, h = x.g * a.G + row % a.G;
         const bool exists = t < a.T;
-        seen[s] = exists ? min(tokens_seen(x.len, x.n, t, a.causal), end) : 0;
+        seen[s] = exists ? min(x.sees(t, a.causal), end) : 0;
         const char *p = a.q + (((size_t)x.b * a.Hq + (exists ? h : x.g * a.G)) * a.T + (exists ? t : 0)) * (2 * kD);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_token(AttendArgs a, Attend
             q[s][k] = *(const bf16x8 *)(p + 2 * ch);
         }
     }
-    const int full = x.n > 0 ? min(tokens_seen(x.len, x.n, 0, a.causal), end) : 0;     // tokens that every row that counts sees
+    const int full = x.n > 0 ? min(x.sees(0, a.causal), end) : 0;     // tokens that every row that counts sees
 
     f32x4 o[kSets][kE];
     float top[kSets], sum[kSets];

@@ -67,3 +67,32 @@ def test_channels_that_are_not_turned_stay_as_they_are(dtype, kind, d, pairs, in
                         codes, byte = oc.e4m3(rows[0, t, h, i:i + 32].double())
                         assert torch.equal(torch.nan_to_num(held[h - Hq, t, i:i + 32], nan=1e9), torch.nan_to_num(codes, nan=1e9))
                         assert int(cache.k_scale[page, h - Hq, t, i // 32]) == int(byte)
+
+
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("d,T", [(64, 5), (128, 5), (128, 40)])
+def test_chunks_that_reach_past_the_end(dtype, kind, d, T):
+    """Rows for which the cache has no room are dropped; every other new token sees itself and what was there before it, those behind
+    the end all of the cache.  Held to the same token alone, over a sequence that ends with it."""
+    B, Hq, Hkv, page, M = 4, 4, 2, 16, 4
+    cap = page * M
+    cache, want = cu.make(kind, B, Hkv, d, page, M, seed=T)
+    g = torch.Generator().manual_seed(T)
+    rows = [torch.randn(B, T, h, d, generator=g).to(cu.DT[dtype]) for h in (Hq, Hkv, Hkv)]
+    lens = [cap + 1, cap + T - 1, cap + T, 2 ** 31 - 1]
+    q = obc.obc_cache_append(cache, rows[1].cuda(), rows[2].cuda(), _i32(*lens), q=rows[0].cuda())
+    held = dict(zip("kv", cu.held(cache)), table=want["table"])
+    for b in range(B):
+        for t in range(T):
+            j = lens[b] - T + t
+            if j < cap and kind != "e4m3":                           # the token's own row lies where its limit says
+                for h in range(Hkv):
+                    assert torch.equal(held["k"][oc.place(held, b, h, j)], rows[1][b, t, h].double())
+    for causal in (True, False):
+        out = obc.obc_attend(q, cache, _i32(*lens), causal=causal)
+        per_head = obc.obc_attend(q, cache, _i32(*([x] * Hkv for x in lens)), causal=causal)
+        assert torch.equal(out, per_head)
+        for t in range(T):
+            ends = torch.tensor([min(x - T + t + 1, cap) if causal else cap for x in lens])
+            ref = oc.attend(q[:, :, t:t + 1].cpu(), held, ends, causal=causal)
+            cu.check_attend(out[:, t:t + 1], ref, cap, d, dtype)
