@@ -385,7 +385,8 @@ int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t 
  *        nothing, are 0.  Must not alias the inputs.
  * Rows of the cache from lens on, pages that only hold such rows, and rows t >= n_b of q may hold anything; NaN or an infinity in the
  * first `lens` rows gives undefined results for that KV head.
- * Products are summed in fp32.  With bf16 queries the weights are rounded to bf16 before they meet v.
+ * Products are summed in fp32.  With bf16 queries the weights are rounded to bf16 before they meet v.  Weights are at most 1 until they are
+ * divided by their sum: results are finite where logits scale * q.k stay below 2^20 and values below 2^127 / lens in magnitude.
  * scale > 0 (1/sqrt(d) is the usual one).  workspace: obc_attend_workspace_bytes(...) bytes, 256-byte aligned (none needed where
  * that is 0).  Calls that may run at the same time need workspaces of their own.
  */

@@ -9,7 +9,10 @@
 namespace obc {
 
 constexpr int kAttendChunkRows = 128;  // rows per workgroup of attend_chunk
-constexpr float kLazy = 8.f;           // log2 of how far a weight may grow past its reference before sums are rescaled
+// A row's weights are 2^(logit - reference), with logits in log2, and at most 1, so that sums of N values below 2^127 / N have a place in fp32.  The
+// reference is set kLazy above the largest logit so far, and moved, with the sums rescaled, when a logit passes it.  In fp32 it is set closer: the largest
+// weights' exponents, logit - reference, are rounded to half an ulp of it, 2^-23 at 2 and 2^-21 at 8, which only a weight that becomes bf16 can bear.
+constexpr float kLazy = 8.f, kLazyFp32 = 2.f;
 constexpr float kNone = -3.0e38f;      // running maximum of a row that has seen nothing: finite, so that differences stay numbers
 
 struct Tile {            // rows r0 .. r0 + size - 1 of KV head g of sequence b

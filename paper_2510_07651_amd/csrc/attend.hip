@@ -101,8 +101,8 @@ __global__ __launch_bounds__(256, 1) void attend_fp32(AttendArgs a, AttendPlan p
 #pragma unroll
         for (int r = 0; r < 16; ++r) most = fmaxf(most, z[r]);
         most = mfma::halves_max(most) * a.scale_log2;
-        if (__any(most > top + kLazy)) {
-            const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
+        if (__any(most > top)) {
+            const float now = fmaxf(top, most + kLazyFp32), shrink = __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= shrink;
 #pragma unroll

@@ -260,8 +260,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, Attend
         };
         // Moves the row's reference if a logit has outgrown it.
         const auto refer = [&](float most) {
-            if (__any(most > top + kLazy)) {
-                const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
+            if (__any(most > top)) {
+                const float now = fmaxf(top, most + kLazy), shrink = __builtin_amdgcn_exp2f(top - now);
                 top = now;
                 sum *= shrink;
 #pragma unroll

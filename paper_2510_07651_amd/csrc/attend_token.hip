@@ -185,8 +185,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_token(AttendArgs a, Attend
             float most = fmaxf(fmaxf(fmaxf(z[s][0][0], z[s][0][1]), fmaxf(z[s][0][2], z[s][0][3])),
                                fmaxf(fmaxf(z[s][1][0], z[s][1][1]), fmaxf(z[s][1][2], z[s][1][3])));
             most = across_rows<MaxOp>(most) * a.scale_log2;
-            if (__any(most > top[s] + kLazy)) {
-                const float now = fmaxf(top[s], most), shrink = __builtin_amdgcn_exp2f(top[s] - now);
+            if (__any(most > top[s])) {
+                const float now = fmaxf(top[s], most + kLazy), shrink = __builtin_amdgcn_exp2f(top[s] - now);
                 top[s] = now;
                 sum[s] *= shrink;
 #pragma unroll

@@ -96,3 +96,22 @@ def test_chunks_that_reach_past_the_end(dtype, kind, d, T):
             ends = torch.tensor([min(x - T + t + 1, cap) if causal else cap for x in lens])
             ref = oc.attend(q[:, :, t:t + 1].cpu(), held, ends, causal=causal)
             cu.check_attend(out[:, t:t + 1], ref, cap, d, dtype)
+
+
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("d,T,Hkv,N,step", [(128, 24, 1, 96, 32), (64, 24, 1, 96, 32), (128, 40, 1, 4000, 32), (128, 1, 64, 600, 128), (64, 7, 64, 600, 128),
+                                            (128, 1, 64, 600, 32), (64, 8, 64, 600, 32)])
+def test_values_near_the_end_of_the_range(dtype, kind, d, T, Hkv, N, step):
+    """Weights are at most 1, so that N of the largest values of 1.5 * 2^e have a sum where N * 1.5 * 2^e has a place, also where logits grow from step to
+    step by a little less than what a reference waits for.  All values are alike, and so are the outputs, to the roundings of the sums and of the
+    result."""
+    e = 127 - math.ceil(math.log2(N))
+    cache, _ = cu.make(kind, 1, Hkv, d, 32, -(-N // 32), seed=3)
+    rows, values = torch.zeros(1, N, Hkv, d), torch.full((1, N, Hkv, d), 1.5 * 2.0 ** e)
+    rows[..., 0] = 5.0 * (torch.arange(N) // step).clamp(max=3)[:, None]     # (5 is 7.2 in log2)
+    obc.obc_cache_append(cache, rows.to(cu.DT[dtype]).cuda(), values.to(cu.DT[dtype]).cuda(), _i32(N))
+    q = torch.zeros(1, 4 * Hkv, T, d, dtype=cu.DT[dtype])
+    q[..., 0] = 1.0
+    out = obc.obc_attend(q.cuda(), cache, _i32(N), causal=False, scale=1.0).double().cpu() / 2.0 ** e
+    rel = (2 * N + 80) * 2.0 ** -24 + cu.HALF[dtype]
+    assert bool(((out - 1.5).abs() <= 1.5 * rel).all()), (float(out.min()), float(out.max()))
