@@ -345,8 +345,8 @@ typedef struct {
 } obc_cache_t;
 
 /* Rows of d contiguous elements at data + b * batch_stride + t * token_stride + h * head_stride (elements; not negative,
- * multiples of 16 bytes; data 16-byte aligned): [B, T, H, d] in any order of its first three dimensions, a slice of a fused
- * projection's output included. */
+ * multiples of 16 bytes, anything for a dimension of size 1; data 16-byte aligned): [B, T, H, d] in any order of its first three
+ * dimensions, a slice of a fused projection's output included. */
 typedef struct {
     const void *data;
     int64_t batch_stride, token_stride, head_stride;

@@ -38,13 +38,14 @@ int check_cache(const obc_cache_t *c, CacheView *view) {
     return OBC_OK;
 }
 
-// Rows of d elements that may be read 16 bytes at a time.
-int check_rows(const obc_rows_t *r, int dtype, RowsView *view) {
+// Rows of d elements that may be read 16 bytes at a time.  The stride of a dimension of size 1 is nobody's: 0 in the view.
+int check_rows(const obc_rows_t *r, int B, int T, int H, int dtype, RowsView *view) {
     if (!r || !r->data || !aligned(r->data, 16)) return OBC_EINVAL;
     const int64_t size = (int64_t)element_bytes(dtype), most = INT64_MAX / 64;
-    for (const int64_t s : {r->batch_stride, r->token_stride, r->head_stride})
+    const int64_t strides[3] = {B > 1 ? r->batch_stride : 0, T > 1 ? r->token_stride : 0, H > 1 ? r->head_stride : 0};
+    for (const int64_t s : strides)
         if (s < 0 || s > most || s * size % 16 != 0) return OBC_EINVAL;
-    *view = {(const char *)r->data, r->batch_stride * size, r->token_stride * size, r->head_stride * size};
+    *view = {(const char *)r->data, strides[0] * size, strides[1] * size, strides[2] * size};
     return OBC_OK;
 }
 
@@ -77,9 +78,9 @@ int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t 
     if (B != cache->batch || T < 1 || !lens) return OBC_EINVAL;
     if (dtype != OBC_F32 && dtype != OBC_BF16) return OBC_EUNSUPPORTED;
     if (cache->dtype != dtype && cache->dtype != OBC_E4M3) return OBC_EUNSUPPORTED;
-    if ((rc = check_rows(k, dtype, &a.k)) != OBC_OK || (rc = check_rows(v, dtype, &a.v)) != OBC_OK) return rc;
+    if ((rc = check_rows(k, B, T, cache->Hkv, dtype, &a.k)) != OBC_OK || (rc = check_rows(v, B, T, cache->Hkv, dtype, &a.v)) != OBC_OK) return rc;
     if (q) {
-        if ((rc = check_rows(q, dtype, &a.q)) != OBC_OK) return rc;
+        if ((rc = check_rows(q, B, T, Hq, dtype, &a.q)) != OBC_OK) return rc;
         if (!q_out || !aligned(q_out, 16) || Hq < 1 || Hq % cache->Hkv != 0) return OBC_EINVAL;
         if (new_lens && new_lens_per_head) return OBC_EINVAL;      // a query belongs to its token, not to a KV head's list
     } else if (q_out || q_norm || Hq != 0) {

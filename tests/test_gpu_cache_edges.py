@@ -115,3 +115,21 @@ def test_values_near_the_end_of_the_range(dtype, kind, d, T, Hkv, N, step):
     out = obc.obc_attend(q.cuda(), cache, _i32(N), causal=False, scale=1.0).double().cpu() / 2.0 ** e
     rel = (2 * N + 80) * 2.0 ** -24 + cu.HALF[dtype]
     assert bool(((out - 1.5).abs() <= 1.5 * rel).all()), (float(out.min()), float(out.max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_strides_of_dimensions_of_size_1(dtype):
+    """One token whose dimension was added behind the channels, one head behind a sequence: the same bits as from rows in order."""
+    B, H, d = 3, 2, 64
+    x = torch.randn(3, B, H, d, generator=torch.Generator().manual_seed(0)).to(cu.DT[dtype]).cuda()
+    odd = [t[:, :, :, None].permute(0, 3, 1, 2) for t in x]            # [B,1,H,d], token stride 1
+    assert odd[0].stride(1) == 1
+    caches = [cu.make(dtype, B, H, d, 16, 2, seed=1)[0] for _ in range(2)]
+    lens = _i32(5, 17, 32)
+    outs = [obc.obc_cache_append(c, k, v, lens, q=q) for c, (q, k, v) in zip(caches, (odd, [t[:, None].contiguous() for t in x]))]
+    assert torch.equal(*outs) and torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v, caches[1].v)
+    single = x[0, :1, 0]                                               # [1,d] as one sequence of one head
+    one = [cu.make(dtype, 1, 1, d, 16, 2, seed=1)[0] for _ in range(2)]
+    for c, rows in zip(one, (single.as_strided((1, 1, 1, d), (7, 3, 5, 1)), single.view(1, 1, 1, d))):
+        obc.obc_cache_append(c, rows, rows, _i32(9))
+    assert torch.equal(one[0].k, one[1].k)
