@@ -400,7 +400,7 @@ int obc_attend(const void *q, const obc_cache_t *cache, void *out, const int32_t
  *   keep_idx      [B, Hkv, n] int32 or NULL (then n <= pages_per_seq * page_size); -1 gives an all-zero row, entries past the
  *                 cache's end are clamped to its last row, as in obc_compact
  *   k_out, v_out  [B, Hkv, n, d] of `dtype`: the cache's own, or OBC_F32 or OBC_BF16 for an OBC_E4M3 cache; n at most
- *                 OBC_MAX_CACHE_ROWS / 8
+ *                 OBC_MAX_CACHE_ROWS / 8.  Must not overlap each other or rows that are read.
  * With the indices of obc_select* it is obc_compact for paged and 8-bit caches; obc_cache_append stores the result again.
  */
 int obc_cache_read(const obc_cache_t *cache, const int32_t *keep_idx, void *k_out, void *v_out, int B, int n, int dtype,

@@ -2,6 +2,7 @@
 // Nothing here allocates or synchronises.
 #include <cmath>
 #include <cstring>
+#include <utility>
 
 #include "cache.h"
 
@@ -47,6 +48,29 @@ int check_rows(const obc_rows_t *r, int B, int T, int H, int dtype, RowsView *vi
         if (s < 0 || s > most || s * size % 16 != 0) return OBC_EINVAL;
     *view = {(const char *)r->data, strides[0] * size, strides[1] * size, strides[2] * size};
     return OBC_OK;
+}
+
+bool overlap(const void *p, const void *q, int64_t p_bytes, int64_t q_bytes) {
+    return (uintptr_t)p < (uintptr_t)q + (uintptr_t)q_bytes && (uintptr_t)q < (uintptr_t)p + (uintptr_t)p_bytes;
+}
+
+// Whether one of the rows (of `row` bytes) meets the `bytes` from `p` on.  Rows that are apart from them as a whole, which is all but every
+// call, cost three products; others are gone through, two dimensions step by step, the longest at once.
+bool meets_rows(const RowsView &r, int B, int T, int H, int64_t row, const void *p, int64_t bytes) {
+    typedef __int128 wide;
+    struct { int64_t n, stride; } dim[3] = {{B, r.batch}, {T, r.token}, {H, r.head}};
+    const wide from = (wide)(uintptr_t)p - (wide)(uintptr_t)r.base, to = from + bytes;
+    if (to <= 0 || from >= (wide)(B - 1) * r.batch + (wide)(T - 1) * r.token + (wide)(H - 1) * r.head + row) return false;
+    if (dim[0].n > dim[2].n) std::swap(dim[0], dim[2]);
+    if (dim[1].n > dim[2].n) std::swap(dim[1], dim[2]);
+    for (int64_t i = 0; i < dim[0].n; ++i)
+        for (int64_t j = 0; j < dim[1].n; ++j) {
+            // the first row that ends behind `from`
+            const wide at = (wide)i * dim[0].stride + (wide)j * dim[1].stride, short_by = from - row + 1 - at;
+            const wide k = short_by <= 0 ? 0 : dim[2].stride == 0 ? dim[2].n : (short_by + dim[2].stride - 1) / dim[2].stride;
+            if (k < dim[2].n && at + k * dim[2].stride < to) return true;
+        }
+    return false;
 }
 
 int attend_plan_of(int B, int T, int Hq, const obc_cache_t *cache, int dtype, CacheView *view, AttendPlan *plan) {
@@ -97,6 +121,12 @@ int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t 
     const bool as_they_are = !q && !rot_pairs && !k_norm;
     if ((long long)B * T >= (as_they_are ? 1LL << 27 : 1LL << 24) || (long long)B * T * (Hq + 2LL * cache->Hkv) > (1LL << 34) || Hq > 65535)
         return OBC_EUNSUPPORTED;
+    if (q) {
+        const int64_t row = cache->d * (int64_t)element_bytes(dtype), out = (int64_t)B * T * Hq * row;
+        if (meets_rows(a.q, B, T, Hq, row, q_out, out) || meets_rows(a.k, B, T, cache->Hkv, row, q_out, out) ||
+            meets_rows(a.v, B, T, cache->Hkv, row, q_out, out))
+            return OBC_EINVAL;
+    }
     a.q_out = (char *)q_out;
     a.lens = {lens, lens_per_head != 0};
     a.fresh = {new_lens, new_lens_per_head != 0};
@@ -132,6 +162,8 @@ int obc_attend(const void *q, const obc_cache_t *cache, void *out, const int32_t
     if (!q || !out || !lens || !aligned(q, 16) || !aligned(out, 16) || !aligned(lens, 4) || !aligned(new_lens, 4)) return OBC_EINVAL;
     if (!(scale > 0.f) || !std::isfinite(scale * 1.4426950408889634f)) return OBC_EINVAL;
     if (plan.total && (!workspace || !aligned(workspace, 256) || workspace_bytes < plan.total)) return OBC_EWORKSPACE;
+    const int64_t rows_bytes = (int64_t)B * T * Hq * cache->d * (int64_t)element_bytes(dtype);
+    if (overlap(q, out, rows_bytes, rows_bytes)) return OBC_EINVAL;
     a.q = (const char *)q;
     a.out = (char *)out;
     a.lens = {lens, lens_per_head != 0};
@@ -153,6 +185,8 @@ int obc_cache_read(const obc_cache_t *cache, const int32_t *keep_idx, void *k_ou
     if (dtype != OBC_F32 && dtype != OBC_BF16) return OBC_EUNSUPPORTED;
     if (cache->dtype != dtype && cache->dtype != OBC_E4M3) return OBC_EUNSUPPORTED;
     if (n > OBC_MAX_CACHE_ROWS / 8 || (long long)B * cache->Hkv * n > (1LL << 34)) return OBC_EUNSUPPORTED;
+    const int64_t out_bytes = (int64_t)B * cache->Hkv * n * cache->d * (int64_t)element_bytes(dtype);
+    if (overlap(k_out, v_out, out_bytes, out_bytes)) return OBC_EINVAL;
     a.keep = keep_idx;
     a.k_out = (char *)k_out;
     a.v_out = (char *)v_out;
