@@ -510,7 +510,8 @@ class KvCache:
 
     k, v [P,Hkv,S,d] float32, bfloat16 or float8_e4m3fn, the latter with k_scale, v_scale [P,Hkv,S,d/32] uint8; page_table [B,M]
     int32, or None: page b is all of sequence b, so that the library's [B,Hkv,N,d] caches serve as they are.  Tensors are
-    checked here, once; the handle keeps them and their addresses."""
+    checked here, once; the handle keeps them and their addresses, so they are written to but not exchanged: other tensors, a
+    table of more pages for one, take a handle of their own."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: Optional[torch.Tensor] = None,
                  k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
@@ -536,15 +537,20 @@ class KvCache:
                 raise ValueError("page_table must be [B,M] int32")
             if S & (S - 1):
                 raise ValueError("pages of a table hold a power of two of rows")
-        self.k, self.v, self.k_scale, self.v_scale, self.page_table = k, v, k_scale, v_scale, page_table
-        self.batch, pages = (P, 1) if page_table is None else tuple(page_table.shape)
-        self.Hkv, self.d, self.dtype, self.device = Hkv, d, k.dtype, k.device
-        self.capacity = pages * S
-        if self.capacity > 1 << 30 or self.batch * Hkv > 65535:
+        batch, pages = (P, 1) if page_table is None else tuple(page_table.shape)
+        if pages * S > 1 << 30 or batch * Hkv > 65535:
             raise ValueError("at most 2^30 rows per sequence and 65535 KV heads over the batch")
-        self._index = k.get_device()
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self._arg = _CacheArg(ptr(k), ptr(v), ptr(k_scale), ptr(v_scale), ptr(page_table), self.batch, P, pages, S, Hkv, d, codes[k.dtype])
+        self.__dict__.update(
+            k=k, v=v, k_scale=k_scale, v_scale=v_scale, page_table=page_table, batch=batch, Hkv=Hkv, d=d, dtype=k.dtype, device=k.device,
+            capacity=pages * S, _index=k.get_device(),
+            _arg=_CacheArg(ptr(k), ptr(v), ptr(k_scale), ptr(v_scale), ptr(page_table), batch, P, pages, S, Hkv, d, codes[k.dtype]))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a cache's tensors are not exchanged: make another KvCache")
+
+    def __delattr__(self, name):
+        raise AttributeError("a cache's tensors are not exchanged: make another KvCache")
 
     @classmethod
     def empty(cls, num_pages: int, Hkv: int, page_size: int, d: int, dtype=torch.bfloat16, page_table=None, device="cuda"):
