@@ -67,7 +67,7 @@ __device__ __forceinline__ void put_row(const CacheView &c, char *pages, uint8_t
 
 // Rows that are stored as they are: 16 of a head per workgroup, so that neighbours in a page (and their scale bytes) are written together; K
 // and V in one launch.
-template <int kD, int kDtype, bool kCodes, bool kPast>
+template <int kD, int kDtype, bool kCodes>
 __global__ __launch_bounds__(kThreads) void store_rows(AppendArgs a) {
     constexpr int kN = kD / 16, kSize = kDtype == OBC_BF16 ? 2 : 4;
     const int t = blockIdx.x * kGroups + threadIdx.x / 16, lo = threadIdx.x % 16 * kN;
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void store_rows(AppendArgs a) {
     load_bytes<kN * kSize>(raw.w, from.base + b * from.batch + t * from.token + g * from.head + lo * kSize);
     float x[kN];
     widen<kN, kDtype == OBC_BF16>(raw, x);
-    put_row<kN, kDtype == OBC_BF16, kCodes, kPast>(a.cache, blockIdx.z == 0 ? a.cache.k : a.cache.v, blockIdx.z == 0 ? a.cache.k_scale : a.cache.v_scale,
+    put_row<kN, kDtype == OBC_BF16, kCodes, false>(a.cache, blockIdx.z == 0 ? a.cache.k : a.cache.v, blockIdx.z == 0 ? a.cache.k_scale : a.cache.v_scale,
                                                    b, g, (long long)device_len(a.lens, b, g, a.cache.Hkv) - n + t, lo, x);
 }
 
@@ -241,18 +241,21 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t stream) {
     const unsigned tokens = (unsigned)(a.B * a.T);
     const unsigned groups = (rows + kGroups - 1) / kGroups;
     const unsigned y = tokens < 1024 ? groups : 1;       // few tokens: every row a group of its own
-    // More than the eight dies' L2 hold is not read from them again.
-    const bool past = (size_t)tokens * rows * a.d * 2 > ((size_t)8 << 20);
     if (!a.Hq && !a.pairs && !a.k_norm) {
         const dim3 grid((a.T + kGroups - 1) / kGroups, a.B * a.cache.Hkv, 2);
         return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
-            if (past) store_rows<dim.value, type.value, codes.value, true><<<grid, kThreads, 0, stream>>>(a);
-            else store_rows<dim.value, type.value, codes.value, false><<<grid, kThreads, 0, stream>>>(a);
+            store_rows<dim.value, type.value, codes.value><<<grid, kThreads, 0, stream>>>(a);
             return hipGetLastError();
         });
     }
+    // bf16 rows are stored past the caches from 8 MiB of them on (us, kept and past, 32/8 heads of 128 channels; 2048, 4096, 8192, 16384 tokens: inputs from
+    // HBM 19.2 and 18.6, 29.9 and 28.7, 50.5 and 48.5, 94.3 and 90.9; from the caches 13.8 and 12.3, 21.5 and 20.5, 35.9 and 35.7, 93.3 and 67.3; with obc_attend behind it
+    // alike to 0.6 of 65 to 560).  fp32 rows, and rows that are stored as they are, not: from HBM the former gain 0.5 of 27.8 (2048 tokens) and lose 4.2 of 20.6
+    // from the caches; of the latter 2048 x 32 heads into 8 bits take 22.1 and 26.1 with the read behind them, 16384 x 8 in fp32 41.0 and 55.7.
+    const bool past = a.dtype == OBC_BF16 && (size_t)tokens * rows * a.d * 2 > ((size_t)8 << 20);
     return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
-        if (past) append_rows<dim.value, type.value, codes.value, true><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
+        constexpr bool kMay = type.value == OBC_BF16;
+        if (kMay && past) append_rows<dim.value, type.value, codes.value, kMay><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
         else append_rows<dim.value, type.value, codes.value, false><<<dim3(tokens, y), kThreads, 0, stream>>>(a);
         return hipGetLastError();
     });
