@@ -198,7 +198,8 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
 
 // Rows of the cache as bf16 or fp32, kPer channels per thread; a head's rows per grid column, K and V in one launch.  (With threads numbered
 // through, the 64-bit divisions that find a row's head cost more than its way: 4 x 8 heads x 2048 bf16 rows 14.4 us, now 12.2, a copy of as many
-// bytes 13.7; x 8192 60.9 and 54.2.)
+// bytes 13.7; x 8192 60.9 and 54.2.)  Stored past the caches at every size: from 4 x 8 heads x 2048 bf16 rows on that takes 7 to 10 % off a read (54.1 and
+// 58.2 us x 8192; of 8-bit rows 40.0 and 47.4) and puts 0 to 3 % on a read with obc_score of 32 rows behind it (133.4 and 129.0; 121.8 and 118.5; x 2048 the same).
 template <int kD, int kDtype, bool kCodes, int kPer>
 __global__ __launch_bounds__(kThreads) void read_rows(ReadArgs a) {
     constexpr int kPieces = kD / kPer, kSize = kDtype == OBC_BF16 ? 2 : 4;
@@ -262,17 +263,15 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t stream) {
 }
 
 hipError_t launch_cache_read(const ReadArgs &a, hipStream_t stream) {
-    // 16 codes per thread where there are rows enough (us, 8 and 16: 4 x 8 heads x 2048 rows 11.2 and 12.6, x 8192 52.4 and 43.3).
-    const int per = a.cache_dtype == OBC_E4M3 && (size_t)a.B * a.cache.Hkv * a.n >= (1u << 17) ? 16 : 8;
+    // 16 codes per thread where there are rows enough (us, 8 and 16: 4 x 8 heads x 2048 rows 11.2 and 12.6, x 8192 52.4 and 43.3).  Not into fp32, where
+    // a store then is a quarter of a thread's 64 bytes and those past the caches are not put together again (8 heads x 16384 rows 32.5 and 95.4).
+    const int per = a.cache_dtype == OBC_E4M3 && a.dtype == OBC_BF16 && (size_t)a.B * a.cache.Hkv * a.n >= (1u << 17) ? 16 : 8;
     const unsigned pieces = (unsigned)a.n * (a.d / per);
     const dim3 grid((pieces + kThreads - 1) / kThreads, a.B * a.cache.Hkv, 2);
     return with_types(a.d, a.dtype, a.cache_dtype, [&](auto dim, auto type, auto codes) {
-        if constexpr (codes.value) {
-            if (per == 16) read_rows<dim.value, type.value, true, 16><<<grid, kThreads, 0, stream>>>(a);
-            else read_rows<dim.value, type.value, true, 8><<<grid, kThreads, 0, stream>>>(a);
-        } else {
-            read_rows<dim.value, type.value, false, 8><<<grid, kThreads, 0, stream>>>(a);
-        }
+        constexpr int kMost = codes.value && type.value == OBC_BF16 ? 16 : 8;
+        if (per == kMost) read_rows<dim.value, type.value, codes.value, kMost><<<grid, kThreads, 0, stream>>>(a);
+        else read_rows<dim.value, type.value, codes.value, 8><<<grid, kThreads, 0, stream>>>(a);
         return hipGetLastError();
     });
 }
