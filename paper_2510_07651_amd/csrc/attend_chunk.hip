@@ -36,8 +36,9 @@ typedef const __attribute__((address_space(4))) int32_t *table_ptr;    // read t
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Brings blocks of 32 rows of K and V into LDS, block i of the share to slot i % kRing.  start(): block 0 is there after the next
-// barrier, and what follows is under way; turn(i), by all waves: block i + 1 is there and block i - 1 may be overwritten; slice(0, i),
-// slice(1, i): what is left to do of step i, between its first matrix ops.
+// barrier, and of 8-bit rows block 1, with block 2 under way; of bf16 rows blocks 1 and 2 as well (the share's first three blocks are waited
+// for together).  turn(i), by all waves: block i + 1 is there and block i - 1 may be overwritten; slice(0, i), slice(1, i): what is left to do
+// of step i, between its first matrix ops.
 template <int kD, bool kCodes>
 struct Loader;
 
