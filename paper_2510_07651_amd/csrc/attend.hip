@@ -201,11 +201,11 @@ size_t align_up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 // to memory and back.  Predicted / measured, us, 32/8 heads: 512 rows over 8192 tokens in two shares 116 / 98, in four 89 / 83; 1024 of 1024
 // in one 29 / 27, in two 39 / 33; 256 over 2048 in four 27 / 29, in eight 30 / 30; four times 300 over 9000 in one 300 / 250, in three 235 / 217
 // (of ragged lengths 226 and 143), in four 256 / 235; 64 over 32768 in 16 65 / 57, in 32 56 / 54.
-// The lengths of a batch are not known here, and finer shares even out unlike ones: the mean of the time for full lengths and of one for
-// lengths spread over the upper three quarters (mean 5/8), whose workgroups take free places as they come.  Beyond 1024 tiles those even out by
-// themselves.  Measured on 12 batches where the two rules differ, full lengths alone and this one (us): full lengths 0.5 to 11 % slower, median 3 %
-// (3 x 333 rows over 12000, 28/4 heads, 230 and 233; 4 x 512 over 20000 685 and 730), unlike lengths 0 to 23 % faster, median 10 % (180 and 162;
-// 486 and 428).
+// The lengths of a batch are not known here, and finer shares even out unlike ones: the mean of the time for full lengths and of one for lengths
+// anywhere below (mean 1/2), whose workgroups take free places as they come.  Beyond 1024 tiles those even out by themselves.  Measured on random
+// batches, 2 to 16 sequences of 7 head layouts, 16 to 2048 new rows over 512 to 32768.  By full lengths alone / by this rule, 12 batches where they
+// differ: full lengths 0.97 (median; 0.86 to 1.03), half of them 0.90, random ones 1.12 (0.96 to 1.67), evenly spread 1.04, one full and the rest an eighth 1.55
+// (0.91 to 2.56).  Mean 1/2 / 5/8, which 1 plan in 23 tells apart, 14 of those: full 1.02 (0.79 to 1.16), half 1.05, random 0.85, even 0.86, one long 0.65.
 static int chunk_shares(long long units, long long rows, int d, int capacity, int batch) {
     const double alone = d == 128 ? 0.79 : 0.54, beside = d == 128 ? 1.05 : 0.69;
     const int blocks = (capacity + 31) / 32;
@@ -217,7 +217,7 @@ static int chunk_shares(long long units, long long rows, int d, int capacity, in
         const int share = (blocks + s - 1) / s;
         double run = rounds * share;
         if (batch > 1 && units <= 1024) {
-            const double unlike = n <= 256 ? alone * share : beside * share * (n <= 512 ? 1.0 : std::max(1.0, 0.625 * (double)n / 512 + 0.5));
+            const double unlike = n <= 256 ? alone * share : beside * share * (n <= 512 ? 1.0 : std::max(1.0, 0.5 * (double)n / 512 + 0.5));
             run = (run + std::min(run, unlike)) / 2;
         }
         const double t = run + 4.0 * ((n + 511) / 512) + (s > 1 ? 3 + (double)rows * s * d * 1.8e-6 : 0);
