@@ -366,7 +366,7 @@ typedef struct {
  * q may be NULL (with q_out, q_norm NULL and Hq 0): rows that are stored as they are, such as those an eviction kept; only then
  * may new_lens be [B, Hkv] (new_lens_per_head = 1: the lists of obc_select_adaptive).
  * `dtype` (OBC_F32 or OBC_BF16) is the inputs'; the cache's is the same or OBC_E4M3.  q_out and the cache must not overlap the
- * inputs.  B * T < 2^24; 2^27 for rows that are stored as they are.
+ * inputs (OBC_EINVAL where q_out meets a row of q, k or v).  B * T < 2^24; 2^27 for rows that are stored as they are.
  */
 int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t *v, const obc_cache_t *cache, void *q_out,
                      const int32_t *lens, int lens_per_head, const int32_t *new_lens, int new_lens_per_head,
@@ -382,7 +382,7 @@ int obc_cache_append(const obc_rows_t *q, const obc_rows_t *k, const obc_rows_t 
  * A negative lens counts as 0.  T = 1 is a decoding step, a larger T a chunk of a prompt.
  *   q    [B, Hq, T, d] of `dtype` (OBC_F32 or OBC_BF16); the cache is of the same type or OBC_E4M3
  *   out  [B, T, Hq, d] of `dtype` (what the output projection takes), written in full: rows t >= n_b, and rows that see
- *        nothing, are 0.  Must not alias the inputs.
+ *        nothing, are 0.  Must not alias the inputs (OBC_EINVAL where it meets q).
  * Rows of the cache from lens on, pages that only hold such rows, and rows t >= n_b of q may hold anything; NaN or an infinity in the
  * first `lens` rows gives undefined results for that KV head.
  * Products are summed in fp32.  With bf16 queries the weights are rounded to bf16 before they meet v.  Weights are at most 1 until they are
@@ -400,7 +400,7 @@ int obc_attend(const void *q, const obc_cache_t *cache, void *out, const int32_t
  *   keep_idx      [B, Hkv, n] int32 or NULL (then n <= pages_per_seq * page_size); -1 gives an all-zero row, entries past the
  *                 cache's end are clamped to its last row, as in obc_compact
  *   k_out, v_out  [B, Hkv, n, d] of `dtype`: the cache's own, or OBC_F32 or OBC_BF16 for an OBC_E4M3 cache; n at most
- *                 OBC_MAX_CACHE_ROWS / 8.  Must not overlap each other or rows that are read.
+ *                 OBC_MAX_CACHE_ROWS / 8.  Must not overlap rows that are read, nor each other (OBC_EINVAL).
  * With the indices of obc_select* it is obc_compact for paged and 8-bit caches; obc_cache_append stores the result again.
  */
 int obc_cache_read(const obc_cache_t *cache, const int32_t *keep_idx, void *k_out, void *v_out, int B, int n, int dtype,

@@ -168,9 +168,9 @@ struct Loader<kD, true> {
 // S^T is token 8 j + 4 half + i, and V's operand takes its tokens in that order.
 //
 // Bound by matrix cores and vector ALUs in turn: 2048 rows over 16384 tokens, 32/8 heads, d = 128, 505 us, 1.02 PFLOP/s, on a card that held
-// 2.08 GHz, 588 us on one that held 1.88; matrix cores busy 47 % of the cycles, vector ALUs 38 %, no bank conflicts.  Two workgroups share a compute unit, so one's vector work may run beside the other's
+// 2.08 GHz, 588 us on one that held 1.88; matrix cores busy 49 % of the cycles, vector ALUs 39 %, no bank conflicts.  Two workgroups share a compute unit, so one's vector work may run beside the other's
 // matrix ops; 64 rows per wave with twice the registers reached 1.02, eight waves that share the ring 1.02.  8-bit rows, 2 x 509 rows over 20011
-// tokens at most, 28/4 heads: 287 us at the lower clock.
+// tokens at most, 28/4 heads: 259 us, at the lower clock 287.
 template <int kD, bool kCodes>
 __global__ __launch_bounds__(kThreads, 2) void attend_chunk(AttendArgs a, AttendPlan plan, float2 *part_ml, float *part_o) {
     using S = Shape<kD>;
