@@ -546,11 +546,17 @@ class KvCache:
             capacity=pages * S, _index=k.get_device(),
             _arg=_CacheArg(ptr(k), ptr(v), ptr(k_scale), ptr(v_scale), ptr(page_table), batch, P, pages, S, Hkv, d, codes[k.dtype]))
 
+    _FIXED = frozenset(("k", "v", "k_scale", "v_scale", "page_table", "batch", "Hkv", "d", "dtype", "device", "capacity", "_index", "_arg"))
+
     def __setattr__(self, name, value):
-        raise AttributeError("a cache's tensors are not exchanged: make another KvCache")
+        if name in self._FIXED:
+            raise AttributeError("a cache's tensors are not exchanged: make another KvCache")
+        object.__setattr__(self, name, value)
 
     def __delattr__(self, name):
-        raise AttributeError("a cache's tensors are not exchanged: make another KvCache")
+        if name in self._FIXED:
+            raise AttributeError("a cache's tensors are not exchanged: make another KvCache")
+        object.__delattr__(self, name)
 
     @classmethod
     def empty(cls, num_pages: int, Hkv: int, page_size: int, d: int, dtype=torch.bfloat16, page_table=None, device="cuda"):
